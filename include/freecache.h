@@ -218,6 +218,73 @@ fc_status fc_refresh(fc_cache *cache, int32_t layer, const void *x, const void *
                      void *out, void *workspace, size_t workspace_bytes, void *stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * A cache held in 4 bits, and the attention that reads it.  The rows of the prompt and of finished blocks are written once and
+ * read by every later step; at 4 bits per value a step reads 133 bytes per row, kv head and K/V pair of head_dim 128 in place of
+ * 512.  A step over it projects into a full-precision fc_cache of ONE layer that all layers share, moves the fresh rows over and
+ * attends here:
+ *   fc_qkv_project_scatter(one, 0, ...);  fc_q4_store_from(q4, layer, one, 0, ...);  fc_q4_attention(q4, layer, ...)
+ *
+ * Format.  A value is an E2M1 number (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) times a power of two 2^e.  Keys: one e per
+ * block of 32 elements of a row, the least one >= -100 with which the block's largest magnitude is at most 6 * 2^e.  Values: one e
+ * per row (all head_dim elements of one kv head), in the same way, >= -40.  x * 2^-e rounds to the nearest number, of two as near to the
+ * one with the even code (0, 1, 2, 4).  A (kv head, row) of which an element of K or V is not finite, or beyond 6 * 2^120 in K or 6 * 2^40 in V, is kept as
+ * "not a number": it reads back as NaN, and what attends to it becomes NaN.
+ * N(0, 1) rows of 128 come back with 18.7 dB (keys) and 18.0 dB (values) signal to noise.
+ *
+ * The handle is like an fc_cache: the same conventions, one stream at a time, one thread at a time; only fc_q4_attention and
+ * fc_q4_read_rows keep nothing in it and may run at the same time as each other.
+ */
+typedef struct fc_q4_cache fc_q4_cache; /* opaque */
+
+/* Bytes of storage of a 4-bit cache with this config, all layers; 0 on bad config.  (Private to the library and a function of the config
+ * alone: it may be copied as a whole.)  dtype is that of the rows that go in, of q and of out. */
+size_t fc_q4_storage_bytes(const fc_config *cfg);
+
+/* Create a handle.  storage: device buffer of fc_q4_storage_bytes() bytes, 16-byte aligned, borrowed for the life of the handle, or NULL to
+ * let the library allocate zero-filled storage that it then owns.  Zeroed storage reads as zeros.  Nothing else is allocated.
+ * Errors: INVALID_ARG, UNSUPPORTED (geometry; more than 65535 batch * n_kv_heads), OOM. */
+fc_status fc_q4_alloc(const fc_config *cfg, void *storage, fc_q4_cache **out);
+
+/* Destroy the handle and free library-owned storage.  The caller must have synchronised every stream that used it.  NULL is accepted. */
+fc_status fc_q4_free(fc_q4_cache *cache);
+
+/* Store rows: row r of every (sequence, kv head) goes to place pos[b][r], or start + r when pos is NULL.  No other row changes.
+ *   k_rows, v_rows  device [B][Hkv][rows][Dh]
+ *   pos  device int32 [B][rows] or NULL.  A negative entry, or one >= max_seq, marks a padded row: it is not stored.  Where a sequence
+ *        lists a place twice the later row is stored.
+ * Errors: INVALID_ARG, BOUNDS (layer; with pos == NULL: start < 0 or start + rows > max_seq), HIP. */
+fc_status fc_q4_store_rows(fc_q4_cache *cache, int32_t layer, const void *k_rows, const void *v_rows, const int32_t *pos,
+                           int32_t start, int32_t rows, void *stream);
+
+/* Store rows out of a layer of a full-precision cache, each to its own place: the rows pos[b][r], or start + r when pos is NULL.
+ * src has the same batch, n_kv_heads, head_dim, max_seq and dtype.
+ * Errors: INVALID_ARG (also: another geometry), BOUNDS, HIP. */
+fc_status fc_q4_store_from(fc_q4_cache *cache, int32_t layer, const fc_cache *src, int32_t src_layer, const int32_t *pos,
+                           int32_t start, int32_t rows, void *stream);
+
+/* Rows [start, start+rows) as the values they stand for (exact in either dtype), k_rows, v_rows device [B][Hkv][rows][Dh].
+ * Errors: INVALID_ARG, BOUNDS, HIP. */
+fc_status fc_q4_read_rows(const fc_q4_cache *cache, int32_t layer, void *k_rows, void *v_rows, int32_t start, int32_t rows,
+                          void *stream);
+
+/* Workspace bytes of fc_q4_attention for windows of up to max_rows rows at any length up to max_seq; 0 on bad arguments or when none is
+ * needed.  A call with less cuts the keys into fewer ranges, with none into one: the roundings of its result may depend on
+ * workspace_bytes. */
+size_t fc_q4_workspace_bytes(const fc_config *cfg, int32_t max_rows);
+
+/* Bidirectional attention of the window's queries over rows [0, kv_len), or over [0, min(kv_lens[b], kv_len)) of sequence b:
+ * as fc_active_attention, with the values that the rows stand for.
+ *   q        device [B][Hq][A][Dh]
+ *   kv_lens  device int32 [B] or NULL; a sequence of length 0 (or less) has zeros in out
+ *   pos      device int32 [B][A] or NULL; rows with a negative entry produce zeros
+ *   out      device [B][A][Hq*Dh]
+ *   workspace  device, 16-byte aligned, may be NULL.  Two calls that overlap in time must not share one.
+ * Rows behind a sequence's length are not looked at: whatever they hold does not matter.
+ * Errors: INVALID_ARG, BOUNDS (layer; kv_len < 1 or > max_seq), UNSUPPORTED (batch * A beyond 2^24), HIP. */
+fc_status fc_q4_attention(const fc_q4_cache *cache, int32_t layer, const void *q, int32_t A, int32_t kv_len, const int32_t *kv_lens,
+                          const int32_t *pos, void *out, void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
  * The rest of the transformer layer on the window rows (Table 1, rows "Output projection (W_out)",
  * "FFN W_1" and "FFN W_2": with FreeCache each is evaluated for the A window rows only, so its cost
  * drops from O(L ...) to O(A ...) exactly like the projections above).  The paper names these
@@ -340,6 +407,35 @@ fc_status fc_unmask_select(const int32_t *tok, const float *conf, const int32_t 
  * Errors: INVALID_ARG, UNSUPPORTED (row size not a multiple of 16 bytes), HIP. */
 fc_status fc_gather_rows(int32_t dtype, const void *table, int32_t rows, int32_t width, const int32_t *idx,
                          int32_t n, void *out, void *stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Sampled fill: instead of the arg-max, a token drawn from the logits' distribution, with the probability it was drawn with as its
+ * confidence (tok and conf are arguments of fc_unmask_select).  Logits come from fc_linear_residual with w_vocab, or from anywhere.
+ *
+ * The entries of a row stand in one order: the larger logit first, the smaller index first among equals.  With z_max the largest
+ * and w_i = exp((z_i - z_max) / temperature), each filter keeps a prefix of that order:
+ *   top_k  the first top_k entries (0: all)
+ *   top_p  of these, the fewest whose w add up to at least top_p times the sum over them (1: all)
+ *   min_p  those with w_i >= min_p (0: all)
+ * and with W the sum of w over the shortest of the prefixes
+ *   tok[m] = the first entry of the order at which the running sum of w exceeds u[m] W,   conf[m] = w[tok[m]] / W.
+ * temperature 0 is the arg-max with conf = softmax(z)[tok] as in fc_lm_head_argmax; top_k, top_p, min_p and u are then not looked at.
+ * Sums are whole numbers, the largest w being 2^(62 - ceil(log2 V)), at most 2^52: the same bits from call to call, whatever else is in the batch,
+ * and w below half a unit (2^-45 at 152064 entries) count as 0.  NaN entries are passed over, -inf ones have w = 0; of several +inf each has w = 1 and
+ * the finite ones 0.  A row of nothing but NaN and -inf gets tok = -1, conf = 0.
+ */
+
+/* Workspace bytes of fc_sample_tokens for this shape; 0 on bad arguments. */
+size_t fc_sample_workspace_bytes(int32_t dtype, int32_t M, int32_t V);
+
+/*   logits  device [M][ld] (element type dtype), of which the first V entries of a row count; ld >= V elements, any alignment of elements
+ *   u       device float [M], uniform in [0, 1); below 0 counts as 0, 1 or more (and NaN) picks the last kept entry.  May be NULL at temperature 0.
+ *   tok  device int32 [M];  conf  device float [M];  workspace  device, 16-byte aligned, >= fc_sample_workspace_bytes(dtype, M, V) bytes
+ * Errors: INVALID_ARG (NULL; M, V < 1; ld < V; temperature < 0 or not finite; top_k < 0; top_p outside (0, 1]; min_p outside [0, 1]),
+ * UNSUPPORTED (V or M beyond 2^24), WORKSPACE, HIP. */
+fc_status fc_sample_tokens(int32_t dtype, const void *logits, int64_t ld, int32_t M, int32_t V, float temperature, int32_t top_k,
+                           float top_p, float min_p, const float *u, int32_t *tok, float *conf, void *workspace,
+                           size_t workspace_bytes, void *stream);
 
 /* ---------------------------------------------------------------------------------------------
  * Guided Diffusion acceptance (section 3.2.2 and Algorithm 1: the diffusion model proposes a token

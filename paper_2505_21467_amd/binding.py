@@ -30,6 +30,8 @@ EXPORTS = (
     "fc_full_layer_workspace_bytes", "fc_full_layer_step",
     "fc_lm_head_workspace_bytes", "fc_lm_head_argmax", "fc_unmask_select", "fc_gather_rows",
     "fc_guided_accept_workspace_bytes", "fc_guided_accept", "fc_kv_similarity",
+    "fc_q4_storage_bytes", "fc_q4_alloc", "fc_q4_free", "fc_q4_store_rows", "fc_q4_store_from", "fc_q4_read_rows",
+    "fc_q4_workspace_bytes", "fc_q4_attention", "fc_sample_workspace_bytes", "fc_sample_tokens",
 )
 
 
@@ -126,6 +128,27 @@ def lib():
                                        sz, vp]
         L.fc_kv_similarity.restype = ctypes.c_int
         L.fc_kv_similarity.argtypes = [vp, i32, vp, vp, i32, i32, vp, vp, vp]
+        L.fc_q4_storage_bytes.restype = sz
+        L.fc_q4_storage_bytes.argtypes = [cfgp]
+        L.fc_q4_alloc.restype = ctypes.c_int
+        L.fc_q4_alloc.argtypes = [cfgp, vp, ctypes.POINTER(vp)]
+        L.fc_q4_free.restype = ctypes.c_int
+        L.fc_q4_free.argtypes = [vp]
+        L.fc_q4_store_rows.restype = ctypes.c_int
+        L.fc_q4_store_rows.argtypes = [vp, i32, vp, vp, vp, i32, i32, vp]
+        L.fc_q4_store_from.restype = ctypes.c_int
+        L.fc_q4_store_from.argtypes = [vp, i32, vp, i32, vp, i32, i32, vp]
+        L.fc_q4_read_rows.restype = ctypes.c_int
+        L.fc_q4_read_rows.argtypes = [vp, i32, vp, vp, i32, i32, vp]
+        L.fc_q4_workspace_bytes.restype = sz
+        L.fc_q4_workspace_bytes.argtypes = [cfgp, i32]
+        L.fc_q4_attention.restype = ctypes.c_int
+        L.fc_q4_attention.argtypes = [vp, i32, vp, i32, i32, vp, vp, vp, vp, sz, vp]
+        L.fc_sample_workspace_bytes.restype = sz
+        L.fc_sample_workspace_bytes.argtypes = [i32, i32, i32]
+        L.fc_sample_tokens.restype = ctypes.c_int
+        L.fc_sample_tokens.argtypes = [i32, vp, ctypes.c_int64, i32, i32, ctypes.c_float, i32, ctypes.c_float,
+                                       ctypes.c_float, vp, vp, vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -329,3 +352,53 @@ def fc_guided_accept(dlm, ar, pos, win_start, B, A, V, topk, tau, mask_id, token
 def fc_kv_similarity(cache, layer, k_prev, v_prev, start, rows, sim_k, sim_v, stream=None) -> None:
     _check(lib().fc_kv_similarity(cache, layer, _ptr(k_prev), _ptr(v_prev), start, rows, _ptr(sim_k), _ptr(sim_v),
                                   _stream(stream)))
+
+
+def fc_q4_storage_bytes(cfg: fc_config) -> int:
+    return int(lib().fc_q4_storage_bytes(ctypes.byref(cfg)))
+
+
+def fc_q4_alloc(cfg: fc_config, storage=None):
+    """Returns an opaque handle (int). A storage tensor, if given, is borrowed: keep it alive."""
+    out = ctypes.c_void_p()
+    _check(lib().fc_q4_alloc(ctypes.byref(cfg), _ptr(storage), ctypes.byref(out)))
+    return out.value
+
+
+def fc_q4_free(cache) -> None:
+    _check(lib().fc_q4_free(cache))
+
+
+def fc_q4_store_rows(cache, layer, k_rows, v_rows, pos, start, rows, stream=None) -> None:
+    _check(lib().fc_q4_store_rows(cache, layer, _ptr(k_rows), _ptr(v_rows), _ptr(pos), start, rows, _stream(stream)))
+
+
+def fc_q4_store_from(cache, layer, src, src_layer, pos, start, rows, stream=None) -> None:
+    _check(lib().fc_q4_store_from(cache, layer, src, src_layer, _ptr(pos), start, rows, _stream(stream)))
+
+
+def fc_q4_read_rows(cache, layer, k_rows, v_rows, start, rows, stream=None) -> None:
+    _check(lib().fc_q4_read_rows(cache, layer, _ptr(k_rows), _ptr(v_rows), start, rows, _stream(stream)))
+
+
+def fc_q4_workspace_bytes(cfg: fc_config, max_rows: int) -> int:
+    return int(lib().fc_q4_workspace_bytes(ctypes.byref(cfg), max_rows))
+
+
+def fc_q4_attention(cache, layer, q, A, kv_len, kv_lens, pos, out, workspace, workspace_bytes=None, stream=None) -> None:
+    if workspace_bytes is None:
+        workspace_bytes = _nbytes(workspace)
+    _check(lib().fc_q4_attention(cache, layer, _ptr(q), A, kv_len, _ptr(kv_lens), _ptr(pos), _ptr(out), _ptr(workspace),
+                                 workspace_bytes, _stream(stream)))
+
+
+def fc_sample_workspace_bytes(dtype, M, V) -> int:
+    return int(lib().fc_sample_workspace_bytes(DTYPE_CODE[dtype], M, V))
+
+
+def fc_sample_tokens(dtype, logits, ld, M, V, temperature, top_k, top_p, min_p, u, tok, conf, workspace,
+                     workspace_bytes=None, stream=None) -> None:
+    if workspace_bytes is None:
+        workspace_bytes = _nbytes(workspace)
+    _check(lib().fc_sample_tokens(DTYPE_CODE[dtype], _ptr(logits), ld, M, V, temperature, top_k, top_p, min_p, _ptr(u),
+                                  _ptr(tok), _ptr(conf), _ptr(workspace), workspace_bytes, _stream(stream)))

@@ -9,6 +9,8 @@
 #include <new>
 
 #include "fc_internal.h"
+#include "fc_q4.h"
+#include "fc_sample.h"
 
 namespace {
 
@@ -1396,6 +1398,220 @@ fc_status fc_kv_similarity(const fc_cache *cache, int32_t layer, const void *k_p
                                            layer_ptr(cache, cache->v, layer), k_prev, v_prev, start, rows, sim_k, sim_v,
                                            (hipStream_t)stream);
     return e == hipSuccess ? FC_OK : hip_fail(e, "similarity launch");
+}
+
+// ---------------------------------------------------------------------------------------------
+// The cache held in 4 bits.
+
+struct fc_q4_cache {
+    fc_config cfg;
+    size_t layer_bytes;
+    uint8_t *storage;
+    bool owned;
+};
+
+namespace {
+
+fc_status check_q4_config(const fc_config *c)
+{
+    fc_status st = check_config(c);
+    if (st != FC_OK) return st;
+    if ((int64_t)c->batch * c->n_kv_heads > 65535) return fail(FC_ERR_UNSUPPORTED, "batch * n_kv_heads is limited to 65535");
+    return FC_OK;
+}
+
+size_t q4_layer_bytes(const fc_config &c)
+{
+    return (size_t)c.batch * c.n_kv_heads * (spad_of(c) / FC_VTILE) * fc_q4_tile_bytes(c.head_dim);
+}
+
+FcQ4Geom q4_geom(const fc_config &c)
+{
+    FcQ4Geom G;
+    G.B = c.batch;
+    G.Hq = c.n_q_heads;
+    G.Hkv = c.n_kv_heads;
+    G.Dh = c.head_dim;
+    G.max_seq = c.max_seq;
+    G.spad = spad_of(c);
+    G.g = c.n_q_heads / c.n_kv_heads;
+    G.dtype = c.dtype;
+    G.scale = c.softmax_scale > 0.f ? c.softmax_scale : (float)(1.0 / sqrt((double)c.head_dim));
+    return G;
+}
+
+fc_status check_q4_layer(const fc_q4_cache *cache, int32_t layer)
+{
+    if (!cache) return fail(FC_ERR_INVALID_ARG, "cache is NULL");
+    if (layer < 0 || layer >= cache->cfg.n_layers)
+        return fail(FC_ERR_BOUNDS, "layer %d outside [0, %d)", layer, cache->cfg.n_layers);
+    return FC_OK;
+}
+
+fc_status check_q4_rows(const fc_q4_cache *cache, bool listed, int32_t start, int32_t rows)
+{
+    if (rows < 1) return fail(FC_ERR_INVALID_ARG, "rows %d must be >= 1", rows);
+    if (rows > (1 << 24)) return fail(FC_ERR_UNSUPPORTED, "rows %d exceeds 2^24", rows);
+    if (!listed && (start < 0 || start > cache->cfg.max_seq - rows))
+        return fail(FC_ERR_BOUNDS, "rows [%d, %d+%d) outside the cache of %d rows", start, start, rows, cache->cfg.max_seq);
+    return FC_OK;
+}
+
+uint8_t *q4_layer(const fc_q4_cache *c, int32_t layer) { return c->storage + (size_t)layer * c->layer_bytes; }
+
+}  // namespace
+
+size_t fc_q4_storage_bytes(const fc_config *cfg)
+{
+    if (check_q4_config(cfg) != FC_OK) return 0;
+    return (size_t)cfg->n_layers * q4_layer_bytes(*cfg);
+}
+
+fc_status fc_q4_alloc(const fc_config *cfg, void *storage, fc_q4_cache **out)
+{
+    fc_status st = check_q4_config(cfg);
+    if (st != FC_OK) return st;
+    if (!out) return fail(FC_ERR_INVALID_ARG, "out is NULL");
+    if ((uintptr_t)storage & 15) return fail(FC_ERR_INVALID_ARG, "storage must be 16-byte aligned");
+    fc_q4_cache *c = new (std::nothrow) fc_q4_cache;
+    if (!c) return fail(FC_ERR_OOM, "host allocation failed");
+    c->cfg = *cfg;
+    c->layer_bytes = q4_layer_bytes(*cfg);
+    c->storage = (uint8_t *)storage;
+    c->owned = !storage;
+    if (!storage) {
+        const size_t bytes = fc_q4_storage_bytes(cfg);
+        void *p = nullptr;
+        if (hipMalloc(&p, bytes) != hipSuccess || hipMemset(p, 0, bytes) != hipSuccess) {
+            (void)hipGetLastError();
+            if (p) (void)hipFree(p);
+            delete c;
+            return fail(FC_ERR_OOM, "could not allocate %zu bytes of cache storage", bytes);
+        }
+        c->storage = (uint8_t *)p;
+    }
+    *out = c;
+    return FC_OK;
+}
+
+fc_status fc_q4_free(fc_q4_cache *cache)
+{
+    if (!cache) return FC_OK;
+    const hipError_t e = cache->owned ? hipFree(cache->storage) : hipSuccess;
+    delete cache;
+    return e == hipSuccess ? FC_OK : hip_fail(e, "hipFree");
+}
+
+fc_status fc_q4_store_rows(fc_q4_cache *cache, int32_t layer, const void *k_rows, const void *v_rows, const int32_t *pos,
+                           int32_t start, int32_t rows, void *stream)
+{
+    fc_status st = check_q4_layer(cache, layer);
+    if (st != FC_OK) return st;
+    if (!k_rows || !v_rows) return fail(FC_ERR_INVALID_ARG, "k_rows or v_rows is NULL");
+    st = check_q4_rows(cache, pos != nullptr, start, rows);
+    if (st != FC_OK) return st;
+    hipError_t e = fc_launch_q4_store(q4_geom(cache->cfg), q4_layer(cache, layer), k_rows, v_rows, pos, start, rows, 0, (hipStream_t)stream);
+    return e == hipSuccess ? FC_OK : hip_fail(e, "4-bit store launch");
+}
+
+fc_status fc_q4_store_from(fc_q4_cache *cache, int32_t layer, const fc_cache *src, int32_t src_layer, const int32_t *pos,
+                           int32_t start, int32_t rows, void *stream)
+{
+    fc_status st = check_q4_layer(cache, layer);
+    if (st == FC_OK) st = check_cache_layer(src, src_layer);
+    if (st != FC_OK) return st;
+    const fc_config &c = cache->cfg, &f = src->cfg;
+    if (c.batch != f.batch || c.n_kv_heads != f.n_kv_heads || c.head_dim != f.head_dim || c.max_seq != f.max_seq || c.dtype != f.dtype)
+        return fail(FC_ERR_INVALID_ARG, "src has another batch, n_kv_heads, head_dim, max_seq or dtype");
+    st = check_q4_rows(cache, pos != nullptr, start, rows);
+    if (st != FC_OK) return st;
+    hipError_t e = fc_launch_q4_store(q4_geom(c), q4_layer(cache, layer), layer_ptr(src, src->k, src_layer), layer_ptr(src, src->v, src_layer),
+                                      pos, start, rows, src->spad, (hipStream_t)stream);
+    return e == hipSuccess ? FC_OK : hip_fail(e, "4-bit store launch");
+}
+
+fc_status fc_q4_read_rows(const fc_q4_cache *cache, int32_t layer, void *k_rows, void *v_rows, int32_t start, int32_t rows,
+                          void *stream)
+{
+    fc_status st = check_q4_layer(cache, layer);
+    if (st != FC_OK) return st;
+    if (!k_rows || !v_rows) return fail(FC_ERR_INVALID_ARG, "k_rows or v_rows is NULL");
+    st = check_q4_rows(cache, false, start, rows);
+    if (st != FC_OK) return st;
+    hipError_t e = fc_launch_q4_read(q4_geom(cache->cfg), q4_layer(cache, layer), k_rows, v_rows, start, rows, (hipStream_t)stream);
+    return e == hipSuccess ? FC_OK : hip_fail(e, "4-bit read launch");
+}
+
+size_t fc_q4_workspace_bytes(const fc_config *cfg, int32_t max_rows)
+{
+    if (check_q4_config(cfg) != FC_OK || max_rows < 1) return 0;
+    return 0;
+}
+
+fc_status fc_q4_attention(const fc_q4_cache *cache, int32_t layer, const void *q, int32_t A, int32_t kv_len, const int32_t *kv_lens,
+                          const int32_t *pos, void *out, void *workspace, size_t workspace_bytes, void *stream)
+{
+    fc_status st = check_q4_layer(cache, layer);
+    if (st != FC_OK) return st;
+    if (!q || !out) return fail(FC_ERR_INVALID_ARG, "q or out is NULL");
+    if (A < 1) return fail(FC_ERR_INVALID_ARG, "A %d must be >= 1", A);
+    if ((int64_t)A * cache->cfg.batch > (1 << 24)) return fail(FC_ERR_UNSUPPORTED, "batch * A exceeds 2^24 rows");
+    if (kv_len < 1 || kv_len > cache->cfg.max_seq)
+        return fail(FC_ERR_BOUNDS, "kv_len %d outside [1, %d]", kv_len, cache->cfg.max_seq);
+    if ((uintptr_t)workspace & 15) return fail(FC_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+    hipError_t e = fc_launch_q4_attention(q4_geom(cache->cfg), q, q4_layer(cache, layer), pos, kv_lens, A, kv_len, out, workspace,
+                                          (hipStream_t)stream);
+    return e == hipSuccess ? FC_OK : hip_fail(e, "4-bit attention launch");
+}
+
+// ---------------------------------------------------------------------------------------------
+// Sampled fill.
+
+size_t fc_sample_workspace_bytes(int32_t dtype, int32_t M, int32_t V)
+{
+    if ((dtype != FC_F32 && dtype != FC_BF16) || M < 1 || V < 1 || M > (1 << 24) || V > (1 << 24)) return 0;
+    return fc_sample_workspace(dtype, M, V);
+}
+
+fc_status fc_sample_tokens(int32_t dtype, const void *logits, int64_t ld, int32_t M, int32_t V, float temperature, int32_t top_k,
+                           float top_p, float min_p, const float *u, int32_t *tok, float *conf, void *workspace,
+                           size_t workspace_bytes, void *stream)
+{
+    fc_status st = check_dtype(dtype);
+    if (st != FC_OK) return st;
+    if (!logits || !tok || !conf) return fail(FC_ERR_INVALID_ARG, "logits, tok or conf is NULL");
+    if (M < 1 || V < 1 || ld < V) return fail(FC_ERR_INVALID_ARG, "M, V >= 1 and ld >= V required");
+    if (!(temperature >= 0.f) || !isfinite(temperature)) return fail(FC_ERR_INVALID_ARG, "temperature must be finite and >= 0");
+    const bool greedy = temperature == 0.f;
+    if (!greedy) {
+        if (!u) return fail(FC_ERR_INVALID_ARG, "u is NULL");
+        if (top_k < 0) return fail(FC_ERR_INVALID_ARG, "top_k %d must be >= 0", top_k);
+        if (!(top_p > 0.f && top_p <= 1.f)) return fail(FC_ERR_INVALID_ARG, "top_p must be in (0, 1]");
+        if (!(min_p >= 0.f && min_p <= 1.f)) return fail(FC_ERR_INVALID_ARG, "min_p must be in [0, 1]");
+    }
+    if (M > (1 << 24) || V > (1 << 24)) return fail(FC_ERR_UNSUPPORTED, "M and V are limited to 2^24");
+    if ((uintptr_t)workspace & 15) return fail(FC_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
+    const size_t need = fc_sample_workspace(dtype, M, V), given = workspace ? workspace_bytes : 0;
+    if (given < need) return fail(FC_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, given);
+    FcSampleArgs p;
+    p.logits = logits;
+    p.ld = ld;
+    p.M = M;
+    p.V = V;
+    p.top_k = greedy || top_k >= V ? 0 : top_k;
+    p.top_p = greedy ? 1.f : top_p;
+    p.min_p = greedy ? 0.f : min_p;
+    p.inv_t = greedy ? 1.0 : 1.0 / (double)temperature;
+    int bits = 62;
+    while (bits > 38 && ((int64_t)1 << (62 - bits)) < V) --bits;
+    p.one = ldexp(1.0, bits < 52 ? bits : 52);  // (whole in fp64)
+    p.greedy = greedy;
+    p.u = u;
+    p.tok = tok;
+    p.conf = conf;
+    p.workspace = workspace;
+    hipError_t e = fc_launch_sample(p, dtype, (hipStream_t)stream);
+    return e == hipSuccess ? FC_OK : hip_fail(e, "sampling launch");
 }
 
 }  // extern "C"

@@ -1,0 +1,20 @@
+// Sampling: arguments handed from the host layer to the kernels.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+struct FcSampleArgs {
+    const void *logits;
+    int64_t ld;  // elements from row to row
+    int32_t M, V, top_k;
+    float top_p, min_p;
+    double inv_t, one;  // 1 / temperature; the whole number that stands for the largest weight
+    int32_t greedy;
+    const float *u;
+    int32_t *tok;
+    float *conf;
+    void *workspace;
+};
+size_t fc_sample_workspace(int dtype, int M, int V);
+hipError_t fc_launch_sample(const FcSampleArgs &p, int dtype, hipStream_t s);
