@@ -124,13 +124,17 @@ bool knob_apply(FcKnobs &k, const char *name, const char *value)
     else if (!strcmp(name, "FC_PROJ_GEMM_SHAPE")) k.proj_gemm_shape = value ? v : d.proj_gemm_shape;
     else if (!strcmp(name, "FC_PROJ_NO_HEADSPLIT")) k.proj_no_headsplit = value ? 1 : 0;
     else if (!strcmp(name, "FC_ACCEPT_WGS")) k.accept_wgs = value ? v : d.accept_wgs;
+    else if (!strcmp(name, "FC_Q4_TILES")) {
+        k.q4_rt = k.q4_waves = k.q4_splits = 0;
+        if (value) sscanf(value, "%d,%d,%d", &k.q4_rt, &k.q4_waves, &k.q4_splits);
+    }
     else return false;
     return true;
 }
 
 const char *const KNOB_NAMES[] = {"FC_ATTN_TILES", "FC_ATTN_WGS", "FC_LIN_WGS", "FC_LIN_NO_ROWS", "FC_LIN_WIDE_SHAPE",
                                   "FC_LIN_KSPLIT", "FC_GEMM_NO_SPLIT", "FC_PROJ_GEMM_SHAPE", "FC_PROJ_NO_HEADSPLIT",
-                                  "FC_ACCEPT_WGS"};
+                                  "FC_ACCEPT_WGS", "FC_Q4_TILES"};
 
 FcKnobs knobs_from_environment()
 {
@@ -1457,6 +1461,19 @@ fc_status check_q4_rows(const fc_q4_cache *cache, bool listed, int32_t start, in
     return FC_OK;
 }
 
+// The most any window of up to max_rows rows can use at any length.
+size_t q4_workspace(const fc_config &c, int32_t max_rows)
+{
+    const FcQ4Geom G = q4_geom(c);
+    size_t most = 0;
+    for (int32_t A = 1; A <= max_rows; A = A < max_rows && 2 * (int64_t)A > max_rows ? max_rows : 2 * A) {
+        const size_t n = fc_q4_plan_workspace(G, fc_plan_q4(G, A, c.max_seq, SIZE_MAX), A);
+        if (n > most) most = n;
+        if (A == max_rows) break;
+    }
+    return most;
+}
+
 uint8_t *q4_layer(const fc_q4_cache *c, int32_t layer) { return c->storage + (size_t)layer * c->layer_bytes; }
 
 }  // namespace
@@ -1545,7 +1562,7 @@ fc_status fc_q4_read_rows(const fc_q4_cache *cache, int32_t layer, void *k_rows,
 size_t fc_q4_workspace_bytes(const fc_config *cfg, int32_t max_rows)
 {
     if (check_q4_config(cfg) != FC_OK || max_rows < 1) return 0;
-    return 0;
+    return q4_workspace(*cfg, max_rows);
 }
 
 fc_status fc_q4_attention(const fc_q4_cache *cache, int32_t layer, const void *q, int32_t A, int32_t kv_len, const int32_t *kv_lens,
@@ -1559,8 +1576,9 @@ fc_status fc_q4_attention(const fc_q4_cache *cache, int32_t layer, const void *q
     if (kv_len < 1 || kv_len > cache->cfg.max_seq)
         return fail(FC_ERR_BOUNDS, "kv_len %d outside [1, %d]", kv_len, cache->cfg.max_seq);
     if ((uintptr_t)workspace & 15) return fail(FC_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
-    hipError_t e = fc_launch_q4_attention(q4_geom(cache->cfg), q, q4_layer(cache, layer), pos, kv_lens, A, kv_len, out, workspace,
-                                          (hipStream_t)stream);
+    const FcQ4Geom G = q4_geom(cache->cfg);
+    const FcQ4Plan plan = fc_plan_q4(G, A, kv_len, workspace ? workspace_bytes : 0);
+    hipError_t e = fc_launch_q4_attention(G, plan, q, q4_layer(cache, layer), pos, kv_lens, A, kv_len, out, workspace, (hipStream_t)stream);
     return e == hipSuccess ? FC_OK : hip_fail(e, "4-bit attention launch");
 }
 

@@ -50,6 +50,7 @@ struct FcKnobs {
     int gemm_no_split;      // FC_GEMM_NO_SPLIT       never cut a GEMM into two launches
     int proj_gemm_shape;    // FC_PROJ_GEMM_SHAPE=0..11 one tile shape for the projection GEMM (-1 = planned)
     int proj_no_headsplit;  // FC_PROJ_NO_HEADSPLIT   short-window projection without the head-split kernels
+    int q4_rt, q4_waves, q4_splits;  // FC_Q4_TILES=R,W,S  row tiles and waves per workgroup, ranges of the attention over 4 bits
     int version;            // changes with every fc_tuning_set
     int accept_wgs;         // FC_ACCEPT_WGS=n        workgroups of the acceptance scan
 };

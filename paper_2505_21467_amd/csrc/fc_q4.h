@@ -45,5 +45,14 @@ struct FcQ4Geom {
 hipError_t fc_launch_q4_store(const FcQ4Geom &G, uint8_t *layer, const void *k, const void *v, const int32_t *pos, int start, int rows,
                               int src_spad, hipStream_t s);
 hipError_t fc_launch_q4_read(const FcQ4Geom &G, const uint8_t *layer, void *k, void *v, int start, int rows, hipStream_t s);
-hipError_t fc_launch_q4_attention(const FcQ4Geom &G, const void *q, const uint8_t *layer, const int32_t *pos, const int32_t *lens, int A, int kv_len,
+
+// Launch plan of the attention (host, pure function of the shape).
+struct FcQ4Plan {
+    int rt;      // 16-row tiles of query rows a workgroup holds
+    int waves;   // its waves
+    int splits;  // ranges the keys are cut into
+};
+FcQ4Plan fc_plan_q4(const FcQ4Geom &G, int A, int kv_len, size_t cap);  // cap: bytes of partial results
+size_t fc_q4_plan_workspace(const FcQ4Geom &G, const FcQ4Plan &p, int A);
+hipError_t fc_launch_q4_attention(const FcQ4Geom &G, const FcQ4Plan &pl, const void *q, const uint8_t *layer, const int32_t *pos, const int32_t *lens, int A, int kv_len,
                                   void *out, void *workspace, hipStream_t s);

@@ -1,11 +1,344 @@
-// Bidirectional attention over a cache held in 4 bits.
+// Bidirectional attention over a cache held in 4 bits (bf16 queries).
+//
+// S^T = K Q^T, softmax weights in registers, O^T = V^T W^T, one pass over the keys.  A wave holds 16 RT query rows (the rows of all
+// query heads that share a kv head are one list) and takes whole tiles of 64 keys, straight from memory into operand registers: the
+// tile's layout is the operands' (fc_q4.h), so the main loop has no LDS, no barrier and no lane crosses.
+//
+//  - Scores.  The 16x16x128 multiply with block scales takes the key codes and their scales as they are stored.  A query row goes in
+//    as two e4m3 parts, the rounded row and 16 times what the rounding left, each with a power of two of its own: together they hold the 8
+//    significant bits of a bfloat16 (elements below 2^-14 of the row's largest lose some, 2^-22 of the largest at most).  Two multiplies at
+//    twice the rate of bfloat16, and no key is ever converted.
+//  - Weights.  Value row t is codes times 2^e_t.  The power goes into the exponent of the row's weight, w_t = 2^(s_t + e_t - r), so the codes
+//    are multiplied as they are, and the sum that divides adds w_t 2^-e_t.  The reference r only has to keep w_t in range: it moves when
+//    a score passes it by 2^8, which after the first tiles is rare.  Weights are rounded to fp16 (11 bits; rounding them to bfloat16 would
+//    add as much error as rounding the output does), sums are fp32.
+//  - Values.  Codes become fp16 pairs by one conversion each, once for all RT row tiles.
+//
+// The waves of a workgroup take tiles in turn and add up in LDS at the end.  Where there are few (sequence, kv head, row group)
+// units, the tiles are cut into ranges, and a second kernel adds their partial results, in fp32.
 #include "fc_device.h"
 #include "fc_internal.h"
 #include "fc_q4.h"
 
 namespace {
 
-// One wave per query row, a key per lane for the scores and an element per lane for the sums: one pass over the keys with the running
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef float f2 __attribute__((ext_vector_type(2)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+typedef int i8x __attribute__((ext_vector_type(8)));
+
+constexpr float MOVE = 8.f;  // a score may pass the reference by 2^MOVE
+
+struct AttnArgs {
+    const bf16_t *q;
+    const uint8_t *layer;
+    const int32_t *pos, *lens;
+    bf16_t *out;
+    float *part;  // partial results: [pair][split][rows][DH], then [pair][split][rows][2] (reference, sum)
+    int A, kv_len, Hq, Hkv, g, tiles, rows, groups, splits, units;
+    float c;  // scale * log2(e)
+    FcDivisor by_groups, by_splits, by_hkv, by_a;
+};
+
+// What a wave loads of a tile.
+template <int DH>
+struct Tile {
+    uint4 k[4], v[DH / 32], vs;
+    uint32_t ks;
+    __device__ __forceinline__ void load(const uint8_t *rec, int lane)
+    {
+        const int kl = DH == 128 ? lane : lane & 31;  // (heads of 64: the upper lanes multiply the same keys with the second part)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) k[t] = *(const uint4 *)(rec + t * (8 * DH) + kl * 16);
+        ks = *(const uint32_t *)(rec + 64 * DH + kl * 4);
+        vs = *(const uint4 *)(rec + fc_q4_vscale(DH) + lane / 16 * 16);
+#pragma unroll
+        for (int j = 0; j < DH / 32; ++j) v[j] = *(const uint4 *)(rec + fc_q4_v(DH) + j * 1024 + lane * 16);
+    }
+};
+
+template <int T>
+__device__ __forceinline__ f4 mul_keys(const uint4 &k, uint32_t ks, const i8x &q, uint32_t qs, f4 acc)
+{
+    const i8x a = {(int)k.x, (int)k.y, (int)k.z, (int)k.w, 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q, acc, 4, 0, T, (int)ks, 0, (int)qs);  // 4: E2M1, 0: e4m3
+}
+
+// Query rows of a wave: the two parts of a row tile and their scales.  Heads of 128: a multiply each; of 64: one multiply, whose first
+// 64 products are the first part's and the other 64 the second's.
+template <int DH, int RT>
+struct Queries {
+    static constexpr int N = DH / 64;
+    i8x part[RT][N];
+    uint32_t scale[RT][N];
+    __device__ __forceinline__ void load(const AttnArgs &p, size_t first, int row0, int lane)
+    {
+        const int m = lane % 16, g = lane / 16;
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            const int row = min(row0 + rt * 16 + m, p.rows - 1);
+            const bf16_t *q = p.q + (first + row) * DH + g * 16;
+            uint4 raw[2 * N];
+#pragma unroll
+            for (int i = 0; i < 2 * N; ++i) raw[i] = fc_load_any<uint4>(q + i / 2 * 64 + i % 2 * 8);
+            float x[16 * N];
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < 16 * N; ++i) {
+                const uint32_t w = ((const uint32_t *)raw)[i / 2];
+                x[i] = __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
+                top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+            }
+            top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+            top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+            const uint32_t e = max(top >> 23, 40u);  // 2^(e - 127) <= largest magnitude < twice that
+            const float inv = __uint_as_float((261 - e) << 23);  // 2^(134 - e): the largest goes to 128 .. 256
+            uint32_t hi[4 * N], lo[4 * N];
+#pragma unroll
+            for (int i = 0; i < 4 * N; ++i) {
+                const float a = x[4 * i] * inv, b = x[4 * i + 1] * inv, c = x[4 * i + 2] * inv, d = x[4 * i + 3] * inv;
+                int u = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+                u = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, u, true);
+                const f2 r = __builtin_amdgcn_cvt_pk_f32_fp8(u, false), s = __builtin_amdgcn_cvt_pk_f32_fp8(u, true);
+                int w = __builtin_amdgcn_cvt_pk_fp8_f32((a - r.x) * 16.f, (b - r.y) * 16.f, 0, false);
+                w = __builtin_amdgcn_cvt_pk_fp8_f32((c - s.x) * 16.f, (d - s.y) * 16.f, w, true);
+                hi[i] = (uint32_t)u;
+                lo[i] = (uint32_t)w;
+            }
+            const bool bad = top >= 0x7f800000u;
+            const uint32_t s_hi = bad ? 255u : e - 7, s_lo = bad ? 255u : e - 11;
+            if constexpr (DH == 128) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    part[rt][0][i] = (int)hi[i];
+                    part[rt][1][i] = (int)lo[i];
+                }
+                scale[rt][0] = s_hi;
+                scale[rt][1] = s_lo;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    part[rt][0][i] = (int)hi[i];
+                    part[rt][0][4 + i] = (int)lo[i];
+                }
+                scale[rt][0] = g < 2 ? s_hi : s_lo;
+            }
+        }
+    }
+};
+
+__device__ __forceinline__ float max16(const f4 (&s)[4])
+{
+    float m = fmaxf(s[0][0], s[0][1]);
+#pragma unroll
+    for (int i = 2; i < 16; i += 2) m = fmaxf(fmaxf(m, s[i / 4][i % 4]), s[i / 4][i % 4 + 1]);
+    return m;
+}
+
+template <int DH, int RT, int W>
+__global__ __launch_bounds__(64 * W) void k_q4_attn(AttnArgs p)
+{
+    constexpr int DT = DH / 16;
+    __shared__ f4 s_o[W][RT][DT][64];
+    __shared__ float s_ref[W][RT * 16], s_sum[W][RT * 16];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int m = lane % 16, g = lane / 16;
+    // Workgroups go to the eight dies in turn: those of one unit (a range of one sequence and kv head) get places 8 apart, so that its row
+    // groups read the tiles through one L2.
+    const uint32_t slot = blockIdx.x >> 3, turn = p.by_groups.over(slot), group = slot - turn * p.groups, unit = turn * 8 + (blockIdx.x & 7);
+    if (unit >= (uint32_t)p.units) return;
+    const uint32_t pair = p.by_splits.over(unit), split = unit - pair * p.splits;
+    const uint32_t b = p.by_hkv.over(pair), j = pair - b * p.Hkv;
+    const int n = p.lens ? min(max(p.lens[b], 0), p.kv_len) : p.kv_len;
+    const int row0 = (int)group * RT * 16;
+    const int all = (n + 63) / 64, per = (all + p.splits - 1) / p.splits;
+    const int from = min(all, (int)split * per), to = min(all, from + per);
+    const uint8_t *rec = p.layer + (size_t)pair * p.tiles * fc_q4_tile_bytes(DH);
+
+    f4 o[DT][RT];
+    float ref[RT], sum[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        ref[rt] = -__builtin_inff();
+        sum[rt] = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) o[dt][rt] = f4{0.f, 0.f, 0.f, 0.f};
+    }
+    Queries<DH, RT> Q;
+    Tile<DH> cur, next;
+    int t = from + wave;
+    if (t < to) next.load(rec + (size_t)t * fc_q4_tile_bytes(DH), lane);
+    Q.load(p, ((size_t)b * p.Hq + (size_t)j * p.g) * p.A, row0, lane);
+    for (; t < to; t += W) {
+        cur = next;
+        if (t + W < to) next.load(rec + (size_t)(t + W) * fc_q4_tile_bytes(DH), lane);
+        float e[16], f[16];  // the rows' exponents (+ 127), and 2^-exponent
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const uint32_t w = ((const uint32_t *)&cur.vs)[i / 4];
+            const uint32_t byte = max(w >> (8 * (i % 4)) & 255, (uint32_t)(FC_Q4_V_LOWEST + 127));  // (rows never stored have 0)
+            e[i] = (float)byte;
+            f[i] = __uint_as_float((254 - byte) << 23);
+        }
+        const bool last = (t + 1) * 64 > n;
+        if (last) {  // rows behind the end may hold anything
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (t * 64 + i / 4 * 16 + g * 4 + i % 4 >= n) f[i] = 0.f;
+        }
+        h8 w[RT][2];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            f4 s[4];
+            const f4 zero = {0.f, 0.f, 0.f, 0.f};
+#define FC_Q4_KEYS(T)                                                                        \
+    s[T] = mul_keys<T>(cur.k[T], cur.ks, Q.part[rt][0], Q.scale[rt][0], zero);               \
+    if constexpr (DH == 128) s[T] = mul_keys<T>(cur.k[T], cur.ks, Q.part[rt][1], Q.scale[rt][1], s[T]);
+            FC_Q4_KEYS(0)
+            FC_Q4_KEYS(1)
+            FC_Q4_KEYS(2)
+            FC_Q4_KEYS(3)
+#undef FC_Q4_KEYS
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i / 4][i % 4] = fmaf(s[i / 4][i % 4], p.c, e[i]);
+            if (last) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (t * 64 + i / 4 * 16 + g * 4 + i % 4 >= n) s[i / 4][i % 4] = -__builtin_inff();
+            }
+            float top = max16(s);
+            if (__any(top > ref[rt] + MOVE)) {
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float r = fmaxf(ref[rt], top), a = __builtin_amdgcn_exp2f(ref[rt] - r);
+                ref[rt] = r;
+                sum[rt] *= a;
+#pragma unroll
+                for (int dt = 0; dt < DT; ++dt) o[dt][rt] *= a;
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float x = __builtin_amdgcn_exp2f(s[i / 4][i % 4] - ref[rt]);
+                sum[rt] = fmaf(x, f[i], sum[rt]);
+                w[rt][i / 8][i % 8] = (_Float16)x;
+            }
+        }
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                const uint32_t c = ((const uint32_t *)&cur.v[dt / 2])[dt % 2 * 2 + kb];
+                h8 v;
+#define FC_Q4_VALUES(B)                                                             \
+    {                                                                               \
+        const h2 x = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4((int)c, 1.0f, B);     \
+        v[2 * B] = x[0];                                                            \
+        v[2 * B + 1] = x[1];                                                        \
+    }
+                FC_Q4_VALUES(0)
+                FC_Q4_VALUES(1)
+                FC_Q4_VALUES(2)
+                FC_Q4_VALUES(3)
+#undef FC_Q4_VALUES
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) o[dt][rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[rt][kb], o[dt][rt], 0, 0, 0);
+            }
+    }
+
+    // The waves' results: every one at the largest reference, added by pieces of 16 rows x 16 elements.
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        float l = sum[rt];
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+        if (g == 0) {
+            s_ref[wave][rt * 16 + m] = ref[rt];
+            s_sum[wave][rt * 16 + m] = l;
+        }
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) s_o[wave][rt][dt][lane] = o[dt][rt];
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int piece = wave; piece < RT * DT; piece += W) {
+        const int rt = piece / DT, dt = piece % DT, row = row0 + rt * 16 + m;
+        if (row >= p.rows) continue;
+        float top = s_ref[0][rt * 16 + m], l = 0.f;
+#pragma unroll
+        for (int i = 1; i < W; ++i) top = fmaxf(top, s_ref[i][rt * 16 + m]);
+        f4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            const float a = from + i < to ? __builtin_amdgcn_exp2f(s_ref[i][rt * 16 + m] - top) : 0.f;
+            l = fmaf(a, s_sum[i][rt * 16 + m], l);
+            x += a * s_o[i][rt][dt][lane];
+        }
+        if (p.splits > 1) {
+            const size_t at = (size_t)unit * p.rows + row;
+            *(f4 *)(p.part + at * DH + dt * 16 + g * 4) = x;
+            if (dt == 0 && g == 0) {
+                float *st = p.part + (size_t)p.units * p.rows * DH + at * 2;
+                st[0] = top;
+                st[1] = l;
+            }
+            continue;
+        }
+        const uint32_t h = p.by_a.over(row), a = row - h * p.A;
+        const bool none = n == 0 || (p.pos && p.pos[(size_t)b * p.A + a] < 0);
+        const float inv = 1.f / l;
+        bf16_t *out = p.out + ((size_t)b * p.A + a) * ((size_t)p.Hq * DH) + (size_t)(j * p.g + h) * DH + dt * 16 + g * 4;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) out[i] = fc_from_float<bf16_t>(none ? 0.f : x[i] * inv);
+    }
+}
+
+// Partial results of the ranges, added at the largest reference; a thread has four elements of a row.
+template <int DH>
+__global__ __launch_bounds__(256) void k_q4_merge(AttnArgs p)
+{
+    constexpr int T = DH / 4;
+    const uint32_t pair = blockIdx.y, b = p.by_hkv.over(pair), j = pair - b * p.Hkv;
+    const int row = blockIdx.x * (256 / T) + threadIdx.x / T, d = threadIdx.x % T * 4;
+    if (row >= p.rows) return;
+    const float *st = p.part + (size_t)p.units * p.rows * DH;
+    const size_t at = (size_t)pair * p.splits * p.rows + row;
+    float top = -__builtin_inff(), l = 0.f;
+    for (int s = 0; s < p.splits; ++s) top = fmaxf(top, st[(at + (size_t)s * p.rows) * 2]);
+    f4 x = {0.f, 0.f, 0.f, 0.f};
+    const int n = p.lens ? min(max(p.lens[b], 0), p.kv_len) : p.kv_len;
+    const int all = (n + 63) / 64, per = (all + p.splits - 1) / p.splits;
+    for (int s = 0; s < p.splits; ++s) {
+        if (s * per >= all) break;
+        const size_t i = at + (size_t)s * p.rows;
+        const float a = __builtin_amdgcn_exp2f(st[i * 2] - top);
+        l = fmaf(a, st[i * 2 + 1], l);
+        x += a * *(const f4 *)(p.part + i * DH + d);
+    }
+    const uint32_t h = p.by_a.over(row), a = row - h * p.A;
+    const bool none = n == 0 || (p.pos && p.pos[(size_t)b * p.A + a] < 0);
+    const float inv = 1.f / l;
+    bf16_t *out = p.out + ((size_t)b * p.A + a) * ((size_t)p.Hq * DH) + (size_t)(j * p.g + h) * DH + d;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = fc_from_float<bf16_t>(none ? 0.f : x[i] * inv);
+}
+
+template <int DH, int RT, int W>
+void launch_w(const AttnArgs &p, hipStream_t s)
+{
+    const unsigned blocks = (unsigned)((p.units + 7) / 8 * 8 * p.groups);
+    k_q4_attn<DH, RT, W><<<dim3(blocks), dim3(64 * W), 0, s>>>(p);
+}
+template <int DH>
+void launch(const AttnArgs &p, const FcQ4Plan &pl, hipStream_t s)
+{
+    if (pl.rt == 4) launch_w<DH, 4, 4>(p, s);
+    else if (pl.rt == 2) pl.waves == 8 ? launch_w<DH, 2, 8>(p, s) : launch_w<DH, 2, 4>(p, s);
+    else pl.waves == 8 ? launch_w<DH, 1, 8>(p, s) : launch_w<DH, 1, 4>(p, s);
+    if (p.splits > 1) k_q4_merge<DH><<<dim3((unsigned)((p.rows + 1024 / DH - 1) / (1024 / DH)), (unsigned)(p.units / p.splits)), dim3(256), 0, s>>>(p);
+}
+
+// One wave per query row (fp32 queries), a key per lane for the scores and an element per lane for the sums: one pass over the keys with the running
 // maximum and sum of the softmax.
 template <typename T, int DH>
 __global__ __launch_bounds__(64) void k_q4_rows(FcQ4Geom G, const T *__restrict__ q, const uint8_t *layer, const int32_t *__restrict__ pos,
@@ -60,16 +393,60 @@ __global__ __launch_bounds__(64) void k_q4_rows(FcQ4Geom G, const T *__restrict_
 
 }  // namespace
 
-hipError_t fc_launch_q4_attention(const FcQ4Geom &G, const void *q, const uint8_t *layer, const int32_t *pos, const int32_t *lens, int A, int kv_len,
-                                  void *out, void *workspace, hipStream_t s)
+size_t fc_q4_plan_workspace(const FcQ4Geom &G, const FcQ4Plan &pl, int A)
 {
-    const dim3 grid((unsigned)A, (unsigned)G.Hq, (unsigned)G.B);
+    return pl.splits > 1 ? (size_t)G.B * G.Hkv * pl.splits * G.g * A * (G.Dh + 2) * sizeof(float) : 0;
+}
+
+FcQ4Plan fc_plan_q4(const FcQ4Geom &G, int A, int kv_len, size_t cap)
+{
+    FcQ4Plan pl{1, 4, 1};
+    if (G.dtype == FC_F32) return pl;
+    const int64_t pairs = (int64_t)G.B * G.Hkv, rows = (int64_t)G.g * A, tiles16 = (rows + 15) / 16;
+    pl.rt = tiles16 <= 1 ? 1 : tiles16 <= 2 ? 2 : 4;
+    pl.waves = 4;
+    if (fc_knobs().q4_rt > 0) pl.rt = fc_knobs().q4_rt, pl.waves = fc_knobs().q4_waves;
+    const int64_t units = pairs * ((tiles16 + pl.rt - 1) / pl.rt), all = (kv_len + 63) / 64;
+    int64_t splits = (256 + units / 2) / units;
+    if (fc_knobs().q4_splits > 0) splits = fc_knobs().q4_splits;
+    splits = splits > all ? all : splits < 1 ? 1 : splits;
+    pl.splits = (int)splits;
+    while (pl.splits > 1 && fc_q4_plan_workspace(G, pl, A) > cap) --pl.splits;
+    return pl;
+}
+
+hipError_t fc_launch_q4_attention(const FcQ4Geom &G, const FcQ4Plan &pl, const void *q, const uint8_t *layer, const int32_t *pos, const int32_t *lens,
+                                  int A, int kv_len, void *out, void *workspace, hipStream_t s)
+{
     if (G.dtype == FC_F32) {
+        const dim3 grid((unsigned)A, (unsigned)G.Hq, (unsigned)G.B);
         if (G.Dh == 128) k_q4_rows<float, 128><<<grid, dim3(64), 0, s>>>(G, (const float *)q, layer, pos, lens, A, kv_len, (float *)out);
         else k_q4_rows<float, 64><<<grid, dim3(64), 0, s>>>(G, (const float *)q, layer, pos, lens, A, kv_len, (float *)out);
-    } else {
-        if (G.Dh == 128) k_q4_rows<bf16_t, 128><<<grid, dim3(64), 0, s>>>(G, (const bf16_t *)q, layer, pos, lens, A, kv_len, (bf16_t *)out);
-        else k_q4_rows<bf16_t, 64><<<grid, dim3(64), 0, s>>>(G, (const bf16_t *)q, layer, pos, lens, A, kv_len, (bf16_t *)out);
+        return hipGetLastError();
     }
+    AttnArgs p;
+    p.q = (const bf16_t *)q;
+    p.layer = layer;
+    p.pos = pos;
+    p.lens = lens;
+    p.out = (bf16_t *)out;
+    p.part = (float *)workspace;
+    p.A = A;
+    p.kv_len = kv_len;
+    p.Hq = G.Hq;
+    p.Hkv = G.Hkv;
+    p.g = G.g;
+    p.tiles = G.spad / FC_VTILE;
+    p.rows = G.g * A;
+    p.groups = (p.rows + 16 * pl.rt - 1) / (16 * pl.rt);
+    p.splits = pl.splits;
+    p.units = G.B * G.Hkv * pl.splits;
+    p.c = G.scale * 1.4426950408889634f;
+    p.by_groups.set((uint32_t)p.groups);
+    p.by_splits.set((uint32_t)p.splits);
+    p.by_hkv.set((uint32_t)p.Hkv);
+    p.by_a.set((uint32_t)A);
+    if (G.Dh == 128) launch<128>(p, pl, s);
+    else launch<64>(p, pl, s);
     return hipGetLastError();
 }

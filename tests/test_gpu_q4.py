@@ -247,6 +247,21 @@ def test_scores_that_grow_and_values_of_many_sizes(dtype, Dh, n):
     c.check(q, hk[:, :, ::-1], hv[:, :, ::-1], n, what="falling")
 
 
+@pytest.mark.parametrize("dtype,Dh", [("bf16", 128), ("bf16", 64), ("f32", 128)])
+def test_rows_never_stored_are_zeros_that_count(dtype, Dh):
+    """Zeroed storage: a row that was never stored has score 0 and value 0, beside rows with large values too."""
+    c = Cache(dtype, 1, 2, 1, Dh, 200)
+    k, v = c.rows(22, 200)
+    v = (v.float() * 2.0 ** 39).to(v.dtype)
+    c.store(k[:, :, 50:120], v[:, :, 50:120], start=50)
+    hk, hv = ref.held_rows(ref.f64(k), ref.f64(v))
+    for x in (hk, hv):
+        x[:, :, :50], x[:, :, 120:] = 0, 0
+    q = inputs.normal(23, "q", (1, 2, 9, Dh), 1.0, dtype)
+    c.check(q, hk, hv, 200, what="rows never stored")
+    assert not Cache(dtype, 1, 2, 1, Dh, 200).attend(q, 200).any()
+
+
 def test_places_that_pass_32_bits():
     """A cache of 2^24 rows: the tiles of the last kv head lie beyond 2^31 bytes, and of the last sequence beyond 2^32."""
     B, Hkv, Dh, S = 2, 2, 128, 1 << 24
