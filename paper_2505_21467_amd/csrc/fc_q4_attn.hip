@@ -37,29 +37,33 @@ struct AttnArgs {
     bf16_t *out;
     float *part;  // partial results: [pair][split][rows][DH], then [pair][split][rows][2] (reference, sum)
     int A, kv_len, Hq, Hkv, g, tiles, rows, groups, splits, units;
-    float c;  // scale * log2(e)
+    float c, by_c;  // scale * log2(e), and 1 / that
     FcDivisor by_groups, by_splits, by_hkv, by_a;
 };
 
-// What a wave loads of a tile.
+// What a wave loads of a tile.  Buffer loads: the place of the tile is a scalar, a lane keeps three offsets.
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 template <int DH>
 struct Tile {
-    uint4 k[4], v[DH / 32], vs;
-    uint32_t ks;
-    __device__ __forceinline__ void load(const uint8_t *rec, int lane)
+    u4 k[4], v[DH / 32];
+    uint32_t ks, vs;
+    __device__ __forceinline__ void load_keys(__amdgpu_buffer_rsrc_t r, uint32_t at, int lane)
     {
         const int kl = DH == 128 ? lane : lane & 31;  // (heads of 64: the upper lanes multiply the same keys with the second part)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) k[t] = *(const uint4 *)(rec + t * (8 * DH) + kl * 16);
-        ks = *(const uint32_t *)(rec + 64 * DH + kl * 4);
-        vs = *(const uint4 *)(rec + fc_q4_vscale(DH) + lane / 16 * 16);
+        for (int t = 0; t < 4; ++t) k[t] = __builtin_amdgcn_raw_buffer_load_b128(r, kl * 16, at + t * (8 * DH), 0);
+        ks = __builtin_amdgcn_raw_buffer_load_b32(r, kl * 4, at + 64 * DH, 0);
+        vs = __builtin_amdgcn_raw_buffer_load_b8(r, lane, at + fc_q4_vscale(DH), 0);
+    }
+    __device__ __forceinline__ void load_values(__amdgpu_buffer_rsrc_t r, uint32_t at, int lane)
+    {
 #pragma unroll
-        for (int j = 0; j < DH / 32; ++j) v[j] = *(const uint4 *)(rec + fc_q4_v(DH) + j * 1024 + lane * 16);
+        for (int j = 0; j < DH / 32; ++j) v[j] = __builtin_amdgcn_raw_buffer_load_b128(r, lane * 16, at + fc_q4_v(DH) + j * 1024, 0);
     }
 };
 
 template <int T>
-__device__ __forceinline__ f4 mul_keys(const uint4 &k, uint32_t ks, const i8x &q, uint32_t qs, f4 acc)
+__device__ __forceinline__ f4 mul_keys(const u4 &k, uint32_t ks, const i8x &q, uint32_t qs, f4 acc)
 {
     const i8x a = {(int)k.x, (int)k.y, (int)k.z, (int)k.w, 0, 0, 0, 0};
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q, acc, 4, 0, T, (int)ks, 0, (int)qs);  // 4: E2M1, 0: e4m3
@@ -137,11 +141,12 @@ __device__ __forceinline__ float max16(const f4 (&s)[4])
 }
 
 template <int DH, int RT, int W>
-__global__ __launch_bounds__(64 * W) void k_q4_attn(AttnArgs p)
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(RT == 4 ? 1 : 2))) void k_q4_attn(AttnArgs p)
 {
     constexpr int DT = DH / 16;
     __shared__ f4 s_o[W][RT][DT][64];
     __shared__ float s_ref[W][RT * 16], s_sum[W][RT * 16];
+    __shared__ __align__(16) float s_start[W][64], s_f[W][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int m = lane % 16, g = lane / 16;
     // Workgroups go to the eight dies in turn: those of one unit (a range of one sequence and kv head) get places 8 apart, so that its row
@@ -154,7 +159,9 @@ __global__ __launch_bounds__(64 * W) void k_q4_attn(AttnArgs p)
     const int row0 = (int)group * RT * 16;
     const int all = (n + 63) / 64, per = (all + p.splits - 1) / p.splits;
     const int from = min(all, (int)split * per), to = min(all, from + per);
-    const uint8_t *rec = p.layer + (size_t)pair * p.tiles * fc_q4_tile_bytes(DH);
+    // (at most 2^18 tiles: offsets fit 32 bits)
+    const uint32_t bytes = (uint32_t)p.tiles * fc_q4_tile_bytes(DH);
+    const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)(p.layer + (size_t)pair * bytes), 0, (int)bytes, 0x00020000);
 
     f4 o[DT][RT];
     float ref[RT], sum[RT];
@@ -166,69 +173,90 @@ __global__ __launch_bounds__(64 * W) void k_q4_attn(AttnArgs p)
         for (int dt = 0; dt < DT; ++dt) o[dt][rt] = f4{0.f, 0.f, 0.f, 0.f};
     }
     Queries<DH, RT> Q;
-    Tile<DH> cur, next;
+    Tile<DH> cur;
     int t = from + wave;
-    if (t < to) next.load(rec + (size_t)t * fc_q4_tile_bytes(DH), lane);
+    if (t < to) {
+        cur.load_keys(rsrc, (uint32_t)t * fc_q4_tile_bytes(DH), lane);
+        cur.load_values(rsrc, (uint32_t)t * fc_q4_tile_bytes(DH), lane);
+    }
     Q.load(p, ((size_t)b * p.Hq + (size_t)j * p.g) * p.A, row0, lane);
+    // The next tile's keys are loaded as soon as these are multiplied, its values likewise.  (Always, the last one once more: behind a
+    // condition the compiler could not tell them from this tile's and would wait for them.)
     for (; t < to; t += W) {
-        cur = next;
-        if (t + W < to) next.load(rec + (size_t)(t + W) * fc_q4_tile_bytes(DH), lane);
-        float e[16], f[16];  // the rows' exponents (+ 127), and 2^-exponent
+        const uint32_t next = (uint32_t)min(t + W, to - 1) * fc_q4_tile_bytes(DH);
+        // The row of this lane's scale byte: exponent / c, where the key multiply starts from, and 2^-exponent; then every lane takes those of
+        // the sixteen rows whose weights it holds.
+        {
+            const float e = (float)max(cur.vs, (uint32_t)(FC_Q4_V_LOWEST + 127)) - 127.f;  // (a row never stored has 0)
+            float start = e * p.by_c, f = __builtin_amdgcn_exp2f(-e);
+            if ((t + 1) * 64 > n) {  // rows behind the end may hold anything: weight 0, and key scales that leave scores finite
+                if (t * 64 + lane % 16 / 4 * 16 + g * 4 + lane % 4 >= n) {
+                    start = -__builtin_inff();
+                    f = 0.f;
+                }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const uint32_t w = ((const uint32_t *)&cur.vs)[i / 4];
-            const uint32_t byte = max(w >> (8 * (i % 4)) & 255, (uint32_t)(FC_Q4_V_LOWEST + 127));  // (rows never stored have 0)
-            e[i] = (float)byte;
-            f[i] = __uint_as_float((254 - byte) << 23);
+                for (int i = 0; i < 4; ++i)
+                    if (t * 64 + i * 16 + m >= n) cur.ks &= ~(0xffu << (8 * i));
+            }
+            s_start[wave][lane] = start;
+            s_f[wave][lane] = f;
         }
-        const bool last = (t + 1) * 64 > n;
-        if (last) {  // rows behind the end may hold anything
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        f4 start[4];
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-                if (t * 64 + i / 4 * 16 + g * 4 + i % 4 >= n) f[i] = 0.f;
-        }
-        h8 w[RT][2];
+        for (int i = 0; i < 4; ++i) start[i] = *(const f4 *)&s_start[wave][g * 16 + i * 4];
+        f4 s[RT][4];
+        bool move = false;
+        float top[RT];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            f4 s[4];
-            const f4 zero = {0.f, 0.f, 0.f, 0.f};
 #define FC_Q4_KEYS(T)                                                                        \
-    s[T] = mul_keys<T>(cur.k[T], cur.ks, Q.part[rt][0], Q.scale[rt][0], zero);               \
-    if constexpr (DH == 128) s[T] = mul_keys<T>(cur.k[T], cur.ks, Q.part[rt][1], Q.scale[rt][1], s[T]);
+    s[rt][T] = mul_keys<T>(cur.k[T], cur.ks, Q.part[rt][0], Q.scale[rt][0], start[T]);       \
+    if constexpr (DH == 128) s[rt][T] = mul_keys<T>(cur.k[T], cur.ks, Q.part[rt][1], Q.scale[rt][1], s[rt][T]);
             FC_Q4_KEYS(0)
             FC_Q4_KEYS(1)
             FC_Q4_KEYS(2)
             FC_Q4_KEYS(3)
 #undef FC_Q4_KEYS
+        }
+        cur.load_keys(rsrc, next, lane);
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[i / 4][i % 4] = fmaf(s[i / 4][i % 4], p.c, e[i]);
-            if (last) {
+        for (int rt = 0; rt < RT; ++rt) {
+            top[rt] = max16(s[rt]) * p.c;
+            move |= top[rt] > ref[rt] + MOVE;
+        }
+        if (__any(move)) {
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (t * 64 + i / 4 * 16 + g * 4 + i % 4 >= n) s[i / 4][i % 4] = -__builtin_inff();
-            }
-            float top = max16(s);
-            if (__any(top > ref[rt] + MOVE)) {
-                top = fmaxf(top, __shfl_xor(top, 16));
-                top = fmaxf(top, __shfl_xor(top, 32));
-                const float r = fmaxf(ref[rt], top), a = __builtin_amdgcn_exp2f(ref[rt] - r);
+            for (int rt = 0; rt < RT; ++rt) {
+                float x = top[rt];
+                x = fmaxf(x, __shfl_xor(x, 16));
+                x = fmaxf(x, __shfl_xor(x, 32));
+                const float r = fmaxf(ref[rt], x), a = __builtin_amdgcn_exp2f(ref[rt] - r);
                 ref[rt] = r;
                 sum[rt] *= a;
 #pragma unroll
                 for (int dt = 0; dt < DT; ++dt) o[dt][rt] *= a;
             }
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float x = __builtin_amdgcn_exp2f(s[i / 4][i % 4] - ref[rt]);
-                sum[rt] = fmaf(x, f[i], sum[rt]);
-                w[rt][i / 8][i % 8] = (_Float16)x;
-            }
         }
+        h8 w[RT][2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f4 f = *(const f4 *)&s_f[wave][g * 16 + i * 4];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float x = __builtin_amdgcn_exp2f(fmaf(s[rt][i][k], p.c, -ref[rt]));
+                    sum[rt] = fmaf(x, f[k], sum[rt]);
+                    w[rt][i / 2][i % 2 * 4 + k] = (_Float16)x;
+                }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
-                const uint32_t c = ((const uint32_t *)&cur.v[dt / 2])[dt % 2 * 2 + kb];
+                const uint32_t c = cur.v[dt / 2][dt % 2 * 2 + kb];
                 h8 v;
 #define FC_Q4_VALUES(B)                                                             \
     {                                                                               \
@@ -244,6 +272,7 @@ __global__ __launch_bounds__(64 * W) void k_q4_attn(AttnArgs p)
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) o[dt][rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[rt][kb], o[dt][rt], 0, 0, 0);
             }
+        cur.load_values(rsrc, next, lane);
     }
 
     // The waves' results: every one at the largest reference, added by pieces of 16 rows x 16 elements.
@@ -442,6 +471,7 @@ hipError_t fc_launch_q4_attention(const FcQ4Geom &G, const FcQ4Plan &pl, const v
     p.splits = pl.splits;
     p.units = G.B * G.Hkv * pl.splits;
     p.c = G.scale * 1.4426950408889634f;
+    p.by_c = 1.f / p.c;
     p.by_groups.set((uint32_t)p.groups);
     p.by_splits.set((uint32_t)p.splits);
     p.by_hkv.set((uint32_t)p.Hkv);
