@@ -1,17 +1,18 @@
 // Bidirectional attention over a cache held in 4 bits (bf16 queries).
 //
 // S^T = K Q^T, softmax weights in registers, O^T = V^T W^T, one pass over the keys.  A wave holds 16 RT query rows (the rows of all
-// query heads that share a kv head are one list) and takes whole tiles of 64 keys, straight from memory into operand registers: the
-// tile's layout is the operands' (fc_q4.h), so the main loop has no LDS, no barrier and no lane crosses.
+// query heads that share a kv head are one list) and takes tiles of 64 keys, straight from memory into operand registers: the
+// tile's layout is the operands' (fc_q4.h), so the main loop has no barrier and, but for 64 scales, no lane crosses.
 //
-//  - Scores.  The 16x16x128 multiply with block scales takes the key codes and their scales as they are stored.  A query row goes in
-//    as two e4m3 parts, the rounded row and 16 times what the rounding left, each with a power of two of its own: together they hold the 8
-//    significant bits of a bfloat16 (elements below 2^-14 of the row's largest lose some, 2^-22 of the largest at most).  Two multiplies at
-//    twice the rate of bfloat16, and no key is ever converted.
+//  - Scores.  The 16x16x128 matrix instruction with block scales takes the key codes and their scales as they are stored; with a 6-bit other operand
+//    it takes 16 clocks, a quarter of what bfloat16 products of that size take.  What a query lacks in bits it gets by parts: a lane's 32
+//    elements of a row are three E2M3 numbers each, every one the rounding error of those before, 2^-16 of the largest of the 32 in the
+//    end (the rows are bfloat16).  48 clocks, and no key is ever converted.  (Two e4m3 parts: 64 clocks.)
 //  - Weights.  Value row t is codes times 2^e_t.  The power goes into the exponent of the row's weight, w_t = 2^(s_t + e_t - r), so the codes
-//    are multiplied as they are, and the sum that divides adds w_t 2^-e_t.  The reference r only has to keep w_t in range: it moves when
-//    a score passes it by 2^8, which after the first tiles is rare.  Weights are rounded to fp16 (11 bits; rounding them to bfloat16 would
-//    add as much error as rounding the output does), sums are fp32.
+//    are multiplied as they are, and the sum that divides adds w_t 2^-e_t.  The key multiply starts from e_t over the softmax scale, so this
+//    costs nothing.  The reference r only has to keep w_t in range: it moves when a score passes it by 2^MOVE, which after the first
+//    tiles is rare.  Weights are rounded to fp16 (11 bits; bfloat16 would add as much error as rounding the output does, two E2M3 parts
+//    more, 2.8e-3 for 1.7e-3 relative in all), sums are fp32.
 //  - Values.  Codes become fp16 pairs by one conversion each, once for all RT row tiles.
 //
 // The waves of a workgroup take tiles in turn and add up in LDS at the end.  Where there are few (sequence, kv head, row group)
@@ -23,10 +24,14 @@
 namespace {
 
 typedef float f4 __attribute__((ext_vector_type(4)));
-typedef float f2 __attribute__((ext_vector_type(2)));
+typedef float f16x __attribute__((ext_vector_type(16)));
+typedef float f32x __attribute__((ext_vector_type(32)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 typedef int i8x __attribute__((ext_vector_type(8)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u6 __attribute__((ext_vector_type(6)));
 
 constexpr float MOVE = 8.f;  // a score may pass the reference by 2^MOVE
 
@@ -42,7 +47,6 @@ struct AttnArgs {
 };
 
 // What a wave loads of a tile.  Buffer loads: the place of the tile is a scalar, a lane keeps three offsets.
-typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 template <int DH>
 struct Tile {
     u4 k[4], v[DH / 32];
@@ -53,7 +57,7 @@ struct Tile {
 #pragma unroll
         for (int t = 0; t < 4; ++t) k[t] = __builtin_amdgcn_raw_buffer_load_b128(r, kl * 16, at + t * (8 * DH), 0);
         ks = __builtin_amdgcn_raw_buffer_load_b32(r, kl * 4, at + 64 * DH, 0);
-        vs = __builtin_amdgcn_raw_buffer_load_b8(r, lane, at + fc_q4_vscale(DH), 0);
+        vs = __builtin_amdgcn_raw_buffer_load_b32(r, lane & ~3, at + fc_q4_vscale(DH), 0);
     }
     __device__ __forceinline__ void load_values(__amdgpu_buffer_rsrc_t r, uint32_t at, int lane)
     {
@@ -62,73 +66,86 @@ struct Tile {
     }
 };
 
-template <int T>
-__device__ __forceinline__ f4 mul_keys(const u4 &k, uint32_t ks, const i8x &q, uint32_t qs, f4 acc)
+// 32 values over `scale` as E2M3, and back.  The even ones come from `a`, the odd ones from `b`.  The instruction writes its first results before
+// it has read its last sources and its scale: they are kept alive behind it, so that the compiler gives it other registers.
+__device__ __forceinline__ u6 to_6bit(const f16x &a, const f16x &b, float scale)
 {
-    const i8x a = {(int)k.x, (int)k.y, (int)k.z, (int)k.w, 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q, acc, 4, 0, T, (int)ks, 0, (int)qs);  // 4: E2M1, 0: e4m3
+    u6 c = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(a, b, scale);
+    asm volatile("" : "+v"(c) : "v"(a), "v"(b), "v"(scale));
+    return c;
+}
+// a, b less what `c` holds of them.
+__device__ __forceinline__ void less_6bit(f16x &a, f16x &b, u6 c, float scale)
+{
+    f32x x = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(c, scale);
+    asm volatile("" : "+v"(x) : "v"(c), "v"(scale));
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        a[i] -= x[2 * i];
+        b[i] -= x[2 * i + 1];
+    }
+}
+__device__ __forceinline__ i8x operand(const u4 &x) { return i8x{(int)x[0], (int)x[1], (int)x[2], (int)x[3], 0, 0, 0, 0}; }
+
+// E2M1 codes times E2M3 ones; SA, SB: the byte of the scales' word.
+template <int SA, int SB>
+__device__ __forceinline__ f4 multiply(const i8x &codes, uint32_t sa, const i8x &part, uint32_t sb, f4 acc)
+{
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(codes, part, acc, 4, 2, SA, (int)sa, SB, (int)sb);
 }
 
-// Query rows of a wave: the two parts of a row tile and their scales.  Heads of 128: a multiply each; of 64: one multiply, whose first
-// 64 products are the first part's and the other 64 the second's.
+// Query rows as operands: N multiplies of a row tile, with the scales in one word.  Heads of 128: three parts, a multiply each.  Heads of 64: the
+// first two parts are the two halves of one multiply (the lower lanes' keys against the first, the upper lanes' against the second), the
+// third one half of another.
 template <int DH, int RT>
 struct Queries {
-    static constexpr int N = DH / 64;
-    i8x part[RT][N];
-    uint32_t scale[RT][N];
-    __device__ __forceinline__ void load(const AttnArgs &p, size_t first, int row0, int lane)
+    static constexpr int N = DH == 128 ? 3 : 2;
+    u4 lo[RT][N][64];
+    u2 hi[RT][N][64];
+    uint32_t scale[RT][64];
+
+    __device__ __forceinline__ void fill(const bf16_t *q, int rt, int lane)  // q: the lane's 32 elements
     {
-        const int m = lane % 16, g = lane / 16;
+        u4 raw[4];
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            const int row = min(row0 + rt * 16 + m, p.rows - 1);
-            const bf16_t *q = p.q + (first + row) * DH + g * 16;
-            uint4 raw[2 * N];
+        for (int i = 0; i < 4; ++i) raw[i] = fc_load_any<u4>(q + i * 8);
+        f16x a, b;
+        uint32_t top = 0;
 #pragma unroll
-            for (int i = 0; i < 2 * N; ++i) raw[i] = fc_load_any<uint4>(q + i / 2 * 64 + i % 2 * 8);
-            float x[16 * N];
-            uint32_t top = 0;
-#pragma unroll
-            for (int i = 0; i < 16 * N; ++i) {
-                const uint32_t w = ((const uint32_t *)raw)[i / 2];
-                x[i] = __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16);
-                top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
-            }
-            top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-            top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-            const uint32_t e = max(top >> 23, 40u);  // 2^(e - 127) <= largest magnitude < twice that
-            const float inv = __uint_as_float((261 - e) << 23);  // 2^(134 - e): the largest goes to 128 .. 256
-            uint32_t hi[4 * N], lo[4 * N];
-#pragma unroll
-            for (int i = 0; i < 4 * N; ++i) {
-                const float a = x[4 * i] * inv, b = x[4 * i + 1] * inv, c = x[4 * i + 2] * inv, d = x[4 * i + 3] * inv;
-                int u = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-                u = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, u, true);
-                const f2 r = __builtin_amdgcn_cvt_pk_f32_fp8(u, false), s = __builtin_amdgcn_cvt_pk_f32_fp8(u, true);
-                int w = __builtin_amdgcn_cvt_pk_fp8_f32((a - r.x) * 16.f, (b - r.y) * 16.f, 0, false);
-                w = __builtin_amdgcn_cvt_pk_fp8_f32((c - s.x) * 16.f, (d - s.y) * 16.f, w, true);
-                hi[i] = (uint32_t)u;
-                lo[i] = (uint32_t)w;
-            }
-            const bool bad = top >= 0x7f800000u;
-            const uint32_t s_hi = bad ? 255u : e - 7, s_lo = bad ? 255u : e - 11;
-            if constexpr (DH == 128) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    part[rt][0][i] = (int)hi[i];
-                    part[rt][1][i] = (int)lo[i];
-                }
-                scale[rt][0] = s_hi;
-                scale[rt][1] = s_lo;
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    part[rt][0][i] = (int)hi[i];
-                    part[rt][0][4 + i] = (int)lo[i];
-                }
-                scale[rt][0] = g < 2 ? s_hi : s_lo;
-            }
+        for (int i = 0; i < 16; ++i) {
+            a[i] = __uint_as_float(raw[i / 4][i % 4] << 16);
+            b[i] = __uint_as_float(raw[i / 4][i % 4] & 0xffff0000u);
+            top = max(top, max(__float_as_uint(a[i]) & 0x7fffffffu, __float_as_uint(b[i]) & 0x7fffffffu));
         }
+        // the largest goes to 4 .. 7.5; below 2^-88 nothing need be exact
+        const uint32_t e = max((top >> 23) + ((top & 0x7fffffu) > 0x700000u ? 1 : 0), 40u) - 2;
+        u6 part[3];
+        part[0] = to_6bit(a, b, __uint_as_float(e << 23));
+        less_6bit(a, b, part[0], __uint_as_float(e << 23));
+        part[1] = to_6bit(a, b, __uint_as_float((e - 4) << 23));  // (at most a quarter of a unit is left: 4 in units of 2^-4)
+        less_6bit(a, b, part[1], __uint_as_float((e - 4) << 23));
+        part[2] = to_6bit(a, b, __uint_as_float((e - 8) << 23));
+        uint32_t s[3] = {e, e - 4, e - 8};
+        if (top >= 0x7f800000u) s[0] = s[1] = s[2] = 255;  // not a number, and neither are the scores
+        if constexpr (DH == 64) {
+            const bool upper = lane >= 32;
+            part[0] = upper ? part[1] : part[0];
+            s[0] = upper ? s[1] : s[0];
+            part[1] = upper ? u6{} : part[2];
+            s[1] = s[2];
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            lo[rt][i][lane] = u4{part[i][0], part[i][1], part[i][2], part[i][3]};
+            hi[rt][i][lane] = u2{part[i][4], part[i][5]};
+        }
+        scale[rt][lane] = s[0] | s[1] << 8 | s[2] << 16;
+    }
+    __device__ __forceinline__ i8x get(int rt, int i, int lane) const
+    {
+        const u4 x = lo[rt][i][lane];
+        const u2 y = hi[rt][i][lane];
+        return i8x{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], 0, 0};
     }
 };
 
@@ -141,10 +158,12 @@ __device__ __forceinline__ float max16(const f4 (&s)[4])
 }
 
 template <int DH, int RT, int W>
-__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(RT == 4 ? 1 : 2))) void k_q4_attn(AttnArgs p)
+__global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) void k_q4_attn(AttnArgs p)
 {
-    constexpr int DT = DH / 16;
+    constexpr int DT = DH / 16, N = Queries<DH, RT>::N;
+    static_assert(RT <= W, "a wave converts one row tile at most");
     __shared__ f4 s_o[W][RT][DT][64];
+    __shared__ Queries<DH, RT> s_q;
     __shared__ float s_ref[W][RT * 16], s_sum[W][RT * 16];
     __shared__ __align__(16) float s_start[W][64], s_f[W][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -172,14 +191,25 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(RT == 4 
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) o[dt][rt] = f4{0.f, 0.f, 0.f, 0.f};
     }
-    Queries<DH, RT> Q;
     Tile<DH> cur;
     int t = from + wave;
     if (t < to) {
         cur.load_keys(rsrc, (uint32_t)t * fc_q4_tile_bytes(DH), lane);
         cur.load_values(rsrc, (uint32_t)t * fc_q4_tile_bytes(DH), lane);
     }
-    Q.load(p, ((size_t)b * p.Hq + (size_t)j * p.g) * p.A, row0, lane);
+    if (wave < RT) {
+        const size_t row = min(row0 + wave * 16 + m, p.rows - 1);
+        s_q.fill(p.q + (((size_t)b * p.Hq + (size_t)j * p.g) * p.A + row) * DH + (DH == 128 ? g : g & 1) * 32, wave, lane);
+    }
+    __syncthreads();
+    i8x q[RT][N];
+    uint32_t qs[RT];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        qs[rt] = s_q.scale[rt][lane];
+#pragma unroll
+        for (int i = 0; i < N; ++i) q[rt][i] = s_q.get(rt, i, lane);
+    }
     // The next tile's keys are loaded as soon as these are multiplied, its values likewise.  (Always, the last one once more: behind a
     // condition the compiler could not tell them from this tile's and would wait for them.)
     for (; t < to; t += W) {
@@ -187,7 +217,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(RT == 4 
         // The row of this lane's scale byte: exponent / c, where the key multiply starts from, and 2^-exponent; then every lane takes those of
         // the sixteen rows whose weights it holds.
         {
-            const float e = (float)max(cur.vs, (uint32_t)(FC_Q4_V_LOWEST + 127)) - 127.f;  // (a row never stored has 0)
+            const float e = (float)max(cur.vs >> (lane % 4 * 8) & 255, (uint32_t)(FC_Q4_V_LOWEST + 127)) - 127.f;  // (a row never stored has 0)
             float start = e * p.by_c, f = __builtin_amdgcn_exp2f(-e);
             if ((t + 1) * 64 > n) {  // rows behind the end may hold anything: weight 0, and key scales that leave scores finite
                 if (t * 64 + lane % 16 / 4 * 16 + g * 4 + lane % 4 >= n) {
@@ -208,17 +238,16 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(RT == 4 
         f4 s[RT][4];
         bool move = false;
         float top[RT];
-#pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-#define FC_Q4_KEYS(T)                                                                        \
-    s[rt][T] = mul_keys<T>(cur.k[T], cur.ks, Q.part[rt][0], Q.scale[rt][0], start[T]);       \
-    if constexpr (DH == 128) s[rt][T] = mul_keys<T>(cur.k[T], cur.ks, Q.part[rt][1], Q.scale[rt][1], s[rt][T]);
-            FC_Q4_KEYS(0)
-            FC_Q4_KEYS(1)
-            FC_Q4_KEYS(2)
-            FC_Q4_KEYS(3)
+// (part by part: products that add to one another are a latency of the matrix core apart)
+#define FC_Q4_KEYS(T, I)                                                                    \
+    _Pragma("unroll") for (int rt = 0; rt < RT; ++rt) s[rt][T] =                              \
+        multiply<T, I>(operand(cur.k[T]), cur.ks, q[rt][I], qs[rt], I == 0 ? start[T] : s[rt][T]);
+#define FC_Q4_PART(I) FC_Q4_KEYS(0, I) FC_Q4_KEYS(1, I) FC_Q4_KEYS(2, I) FC_Q4_KEYS(3, I)
+        FC_Q4_PART(0)
+        FC_Q4_PART(1)
+        if constexpr (N == 3) { FC_Q4_PART(2) }
+#undef FC_Q4_PART
 #undef FC_Q4_KEYS
-        }
         cur.load_keys(rsrc, next, lane);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
@@ -361,8 +390,7 @@ void launch_w(const AttnArgs &p, hipStream_t s)
 template <int DH>
 void launch(const AttnArgs &p, const FcQ4Plan &pl, hipStream_t s)
 {
-    if (pl.rt == 4) launch_w<DH, 4, 4>(p, s);
-    else if (pl.rt == 2) pl.waves == 8 ? launch_w<DH, 2, 8>(p, s) : launch_w<DH, 2, 4>(p, s);
+    if (pl.rt == 2) pl.waves == 8 ? launch_w<DH, 2, 8>(p, s) : launch_w<DH, 2, 4>(p, s);
     else pl.waves == 8 ? launch_w<DH, 1, 8>(p, s) : launch_w<DH, 1, 4>(p, s);
     if (p.splits > 1) k_q4_merge<DH><<<dim3((unsigned)((p.rows + 1024 / DH - 1) / (1024 / DH)), (unsigned)(p.units / p.splits)), dim3(256), 0, s>>>(p);
 }
@@ -432,7 +460,7 @@ FcQ4Plan fc_plan_q4(const FcQ4Geom &G, int A, int kv_len, size_t cap)
     FcQ4Plan pl{1, 4, 1};
     if (G.dtype == FC_F32) return pl;
     const int64_t pairs = (int64_t)G.B * G.Hkv, rows = (int64_t)G.g * A, tiles16 = (rows + 15) / 16;
-    pl.rt = tiles16 <= 1 ? 1 : tiles16 <= 2 ? 2 : 4;
+    pl.rt = tiles16 <= 1 ? 1 : 2;
     pl.waves = 4;
     if (fc_knobs().q4_rt > 0) pl.rt = fc_knobs().q4_rt, pl.waves = fc_knobs().q4_waves;
     const int64_t units = pairs * ((tiles16 + pl.rt - 1) / pl.rt), all = (kv_len + 63) / 64;
