@@ -1461,19 +1461,6 @@ fc_status check_q4_rows(const fc_q4_cache *cache, bool listed, int32_t start, in
     return FC_OK;
 }
 
-// The most any window of up to max_rows rows can use at any length.
-size_t q4_workspace(const fc_config &c, int32_t max_rows)
-{
-    const FcQ4Geom G = q4_geom(c);
-    size_t most = 0;
-    for (int32_t A = 1; A <= max_rows; A = A < max_rows && 2 * (int64_t)A > max_rows ? max_rows : 2 * A) {
-        const size_t n = fc_q4_plan_workspace(G, fc_plan_q4(G, A, c.max_seq, SIZE_MAX), A);
-        if (n > most) most = n;
-        if (A == max_rows) break;
-    }
-    return most;
-}
-
 uint8_t *q4_layer(const fc_q4_cache *c, int32_t layer) { return c->storage + (size_t)layer * c->layer_bytes; }
 
 }  // namespace
@@ -1562,7 +1549,7 @@ fc_status fc_q4_read_rows(const fc_q4_cache *cache, int32_t layer, void *k_rows,
 size_t fc_q4_workspace_bytes(const fc_config *cfg, int32_t max_rows)
 {
     if (check_q4_config(cfg) != FC_OK || max_rows < 1) return 0;
-    return q4_workspace(*cfg, max_rows);
+    return fc_q4_most_workspace(q4_geom(*cfg), max_rows);
 }
 
 fc_status fc_q4_attention(const fc_q4_cache *cache, int32_t layer, const void *q, int32_t A, int32_t kv_len, const int32_t *kv_lens,

@@ -54,5 +54,6 @@ struct FcQ4Plan {
 };
 FcQ4Plan fc_plan_q4(const FcQ4Geom &G, int A, int kv_len, size_t cap);  // cap: bytes of partial results
 size_t fc_q4_plan_workspace(const FcQ4Geom &G, const FcQ4Plan &p, int A);
+size_t fc_q4_most_workspace(const FcQ4Geom &G, int max_rows);
 hipError_t fc_launch_q4_attention(const FcQ4Geom &G, const FcQ4Plan &pl, const void *q, const uint8_t *layer, const int32_t *pos, const int32_t *lens, int A, int kv_len,
                                   void *out, void *workspace, hipStream_t s);

@@ -17,6 +17,9 @@
 //
 // The waves of a workgroup take tiles in turn and add up in LDS at the end.  Where there are few (sequence, kv head, row group)
 // units, the tiles are cut into ranges, and a second kernel adds their partial results, in fp32.
+#include <math.h>
+#include <string.h>
+
 #include "fc_device.h"
 #include "fc_internal.h"
 #include "fc_q4.h"
@@ -176,7 +179,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
     const uint32_t b = p.by_hkv.over(pair), j = pair - b * p.Hkv;
     const int n = p.lens ? min(max(p.lens[b], 0), p.kv_len) : p.kv_len;
     const int row0 = (int)group * RT * 16;
-    const int all = (n + 63) / 64, per = (all + p.splits - 1) / p.splits;
+    const int all = (n + 63) / 64, per = (int)p.by_splits.over((uint32_t)(all + p.splits - 1));
     const int from = min(all, (int)split * per), to = min(all, from + per);
     // (at most 2^18 tiles: offsets fit 32 bits)
     const uint32_t bytes = (uint32_t)p.tiles * fc_q4_tile_bytes(DH);
@@ -346,39 +349,63 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
         const bool none = n == 0 || (p.pos && p.pos[(size_t)b * p.A + a] < 0);
         const float inv = 1.f / l;
         bf16_t *out = p.out + ((size_t)b * p.A + a) * ((size_t)p.Hq * DH) + (size_t)(j * p.g + h) * DH + dt * 16 + g * 4;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) out[i] = fc_from_float<bf16_t>(none ? 0.f : x[i] * inv);
+        uint2 packed;
+        packed.x = fc_bf16_bits(none ? 0.f : x[0] * inv) | (uint32_t)fc_bf16_bits(none ? 0.f : x[1] * inv) << 16;
+        packed.y = fc_bf16_bits(none ? 0.f : x[2] * inv) | (uint32_t)fc_bf16_bits(none ? 0.f : x[3] * inv) << 16;
+        fc_store_any(out, packed);
     }
 }
 
-// Partial results of the ranges, added at the largest reference; a thread has four elements of a row.
+// Partial results of the ranges, added at the largest reference; a thread has four elements of a row.  Eight ranges at a time, all their loads
+// in flight together (one by one a range took 0.37 us).
 template <int DH>
 __global__ __launch_bounds__(256) void k_q4_merge(AttnArgs p)
 {
-    constexpr int T = DH / 4;
+    constexpr int T = DH / 4, N = 8;
     const uint32_t pair = blockIdx.y, b = p.by_hkv.over(pair), j = pair - b * p.Hkv;
     const int row = blockIdx.x * (256 / T) + threadIdx.x / T, d = threadIdx.x % T * 4;
     if (row >= p.rows) return;
-    const float *st = p.part + (size_t)p.units * p.rows * DH;
+    const float2 *st = (const float2 *)(p.part + (size_t)p.units * p.rows * DH);
     const size_t at = (size_t)pair * p.splits * p.rows + row;
-    float top = -__builtin_inff(), l = 0.f;
-    for (int s = 0; s < p.splits; ++s) top = fmaxf(top, st[(at + (size_t)s * p.rows) * 2]);
-    f4 x = {0.f, 0.f, 0.f, 0.f};
-    const int n = p.lens ? min(max(p.lens[b], 0), p.kv_len) : p.kv_len;
-    const int all = (n + 63) / 64, per = (all + p.splits - 1) / p.splits;
-    for (int s = 0; s < p.splits; ++s) {
-        if (s * per >= all) break;
-        const size_t i = at + (size_t)s * p.rows;
-        const float a = __builtin_amdgcn_exp2f(st[i * 2] - top);
-        l = fmaf(a, st[i * 2 + 1], l);
-        x += a * *(const f4 *)(p.part + i * DH + d);
-    }
     const uint32_t h = p.by_a.over(row), a = row - h * p.A;
+    const int n = p.lens ? min(max(p.lens[b], 0), p.kv_len) : p.kv_len;
     const bool none = n == 0 || (p.pos && p.pos[(size_t)b * p.A + a] < 0);
+    const int all = (n + 63) / 64, per = max((int)p.by_splits.over((uint32_t)(all + p.splits - 1)), 1);
+    const int used = (all + per - 1) / per;  // (of a short sequence the last ranges are empty)
+    float top = -__builtin_inff(), l = 0.f;
+    f4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int s0 = 0; s0 < used; s0 += N) {
+        float2 state[N];
+        f4 v[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const size_t k = at + (size_t)min(s0 + i, used - 1) * p.rows;
+            state[i] = st[k];
+            v[i] = *(const f4 *)(p.part + k * DH + d);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        float next = top;
+#pragma unroll
+        for (int i = 0; i < N; ++i) next = fmaxf(next, state[i].x);
+        const float old = s0 ? __builtin_amdgcn_exp2f(top - next) : 0.f;
+        l *= old;
+        x *= old;
+        top = next;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if (s0 + i >= used) continue;
+            const float w = __builtin_amdgcn_exp2f(state[i].x - top);
+            l = fmaf(w, state[i].y, l);
+            x += w * v[i];
+        }
+    }
     const float inv = 1.f / l;
     bf16_t *out = p.out + ((size_t)b * p.A + a) * ((size_t)p.Hq * DH) + (size_t)(j * p.g + h) * DH + d;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = fc_from_float<bf16_t>(none ? 0.f : x[i] * inv);
+    uint2 packed;
+    packed.x = fc_bf16_bits(none ? 0.f : x[0] * inv) | (uint32_t)fc_bf16_bits(none ? 0.f : x[1] * inv) << 16;
+    packed.y = fc_bf16_bits(none ? 0.f : x[2] * inv) | (uint32_t)fc_bf16_bits(none ? 0.f : x[3] * inv) << 16;
+    fc_store_any(out, packed);
 }
 
 template <int DH, int RT, int W>
@@ -455,21 +482,103 @@ size_t fc_q4_plan_workspace(const FcQ4Geom &G, const FcQ4Plan &pl, int A)
     return pl.splits > 1 ? (size_t)G.B * G.Hkv * pl.splits * G.g * A * (G.Dh + 2) * sizeof(float) : 0;
 }
 
+namespace {
+
+constexpr int MOST_SPLITS = 64, MOST_WGS = 512;  // of a call that cuts the keys (more never came out best)
+const int SPLITS[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64};
+
+// What a workgroup shape takes (us): start and end; a tile of a wave; a tile of a compute unit, its loads and multiplies; a workgroup of a compute
+// unit; a second kernel, each range of it, and a MB of partial results.  `part`: what a last partly filled round costs at least.
+struct Q4Shape {
+    int rt, waves;
+    double start, wave, unit, wg, merge, range, mb, part;
+};
+const Q4Shape Q4_128[] = {{1, 4, 4.06, 0.650, 0.157, 0.65, 2.28, 0.077, 0.372, 0.59},
+                          {1, 8, 3.47, 1.047, 0.158, 2.14, 2.10, 0.076, 0.434, 0.75},
+                          {2, 4, 4.87, 0.920, 0.235, 1.43, 2.26, 0.087, 0.312, 0.70},
+                          {2, 8, 4.11, 1.588, 0.244, 2.84, 2.19, 0.082, 0.386, 1.0}};
+const Q4Shape Q4_64[] = {{1, 4, 3.77, 0.476, 0.098, 0.25, 2.13, 0.085, 0.404, 1.0},
+                         {1, 8, 3.61, 0.757, 0.094, 0.74, 2.13, 0.082, 0.516, 0.65},
+                         {2, 4, 4.49, 0.694, 0.161, 0.0, 2.05, 0.088, 0.606, 0.88},
+                         {2, 8, 3.85, 1.161, 0.167, 0.98, 2.14, 0.066, 1.002, 0.92}};
+
+// Estimated time of a call: the longest of a wave's chain of tiles, a compute unit's tiles and the stream from HBM, joined by a 4-norm, and the rest.
+// The load of a compute unit is that of the die with the most units.  Fitted to 2344 measured (shape, plan) pairs of 110 shapes (1 .. 8 sequences, 1 ..
+// 32 kv heads, 1 .. 8 query heads each, 1 .. 256 rows, 16 .. 16800 keys from HBM; rms error 4 .. 8 %); the plan it picks is 1.2 %
+// slower than the best measured one in the mean, 13 % at most.
+double q4_cost(const Q4Shape &sh, int64_t pairs, int64_t rows, int64_t tiles, int dh, int64_t splits)
+{
+    const int64_t groups = (rows + 16 * sh.rt - 1) / (16 * sh.rt), per = (tiles + splits - 1) / splits;
+    double load = (double)((pairs * splits + 7) / 8 * groups) / 32.0;
+    if (load > 1.0) {
+        const double whole = floor(load);
+        if (load > whole) load = whole + sh.part + (1.0 - sh.part) * (load - whole);
+    }
+    const double wave = sh.wave * (double)((per + sh.waves - 1) / sh.waves), unit = sh.unit * load * (double)per;
+    const double hbm = (double)pairs * (double)tiles * (66.0 * dh + 64.0) / 5.5e6;
+    const double w2 = wave * wave, u2 = unit * unit, h2 = hbm * hbm;
+    double us = sh.start + sqrt(sqrt(w2 * w2 + u2 * u2 + h2 * h2)) + sh.wg * load;
+    if (splits > 1) us += sh.merge + sh.range * (double)splits + sh.mb * (double)(pairs * rows * splits * dh) * 4e-6;
+    return us;
+}
+
+FcQ4Plan plan(const FcQ4Geom &G, int A, int kv_len, size_t cap)
+{
+    const int64_t pairs = (int64_t)G.B * G.Hkv, rows = (int64_t)G.g * A, tiles = ((int64_t)kv_len + FC_VTILE - 1) / FC_VTILE;
+    FcQ4Plan best{1, 4, 1};
+    const FcKnobs &k = fc_knobs();
+    if (k.q4_rt > 0) {  // a tuning knob asks for one
+        best = FcQ4Plan{k.q4_rt == 2 ? 2 : 1, k.q4_waves == 8 ? 8 : 4, k.q4_splits > 0 ? k.q4_splits : 1};
+        if (best.splits > tiles) best.splits = (int)tiles;
+        while (best.splits > 1 && fc_q4_plan_workspace(G, best, A) > cap) --best.splits;
+        return best;
+    }
+    double least = 1e30;
+    for (const Q4Shape &sh : G.Dh == 128 ? Q4_128 : Q4_64) {
+        const int64_t groups = (rows + 16 * sh.rt - 1) / (16 * sh.rt);
+        for (const int splits : SPLITS) {
+            const FcQ4Plan pl{sh.rt, sh.waves, splits};
+            if (splits > 1 && (splits > tiles || pairs * groups * splits > MOST_WGS || fc_q4_plan_workspace(G, pl, A) > cap)) break;
+            const double us = q4_cost(sh, pairs, rows, tiles, G.Dh, splits);
+            if (us < least) {
+                least = us;
+                best = pl;
+            }
+        }
+    }
+    return best;
+}
+
+}  // namespace
+
+// Upper bound of what a plan for up to max_rows rows uses: 64 ranges of every row, or 512 workgroups of 32 rows.
+size_t fc_q4_most_workspace(const FcQ4Geom &G, int max_rows)
+{
+    if (G.dtype == FC_F32 || G.spad <= FC_VTILE) return 0;
+    const int64_t rows = (int64_t)G.B * G.Hkv * G.g * max_rows * MOST_SPLITS, most = (int64_t)MOST_WGS * 32;
+    return (size_t)(rows < most ? rows : most) * (G.Dh + 2) * sizeof(float);
+}
+
 FcQ4Plan fc_plan_q4(const FcQ4Geom &G, int A, int kv_len, size_t cap)
 {
-    FcQ4Plan pl{1, 4, 1};
-    if (G.dtype == FC_F32) return pl;
-    const int64_t pairs = (int64_t)G.B * G.Hkv, rows = (int64_t)G.g * A, tiles16 = (rows + 15) / 16;
-    pl.rt = tiles16 <= 1 ? 1 : 2;
-    pl.waves = 4;
-    if (fc_knobs().q4_rt > 0) pl.rt = fc_knobs().q4_rt, pl.waves = fc_knobs().q4_waves;
-    const int64_t units = pairs * ((tiles16 + pl.rt - 1) / pl.rt), all = (kv_len + 63) / 64;
-    int64_t splits = (256 + units / 2) / units;
-    if (fc_knobs().q4_splits > 0) splits = fc_knobs().q4_splits;
-    splits = splits > all ? all : splits < 1 ? 1 : splits;
-    pl.splits = (int)splits;
-    while (pl.splits > 1 && fc_q4_plan_workspace(G, pl, A) > cap) --pl.splits;
-    return pl;
+    if (G.dtype == FC_F32) return FcQ4Plan{1, 4, 1};
+    const size_t most = fc_q4_most_workspace(G, A);
+    if (cap > most && !fc_knobs().q4_rt) cap = most;  // (more changes nothing)
+    // The last few plans of this thread: a program calls with one shape for every layer.
+    struct Entry {
+        int key[7];
+        size_t cap;
+        FcQ4Plan plan;
+    };
+    static thread_local Entry known[4];
+    static thread_local unsigned next = 0;
+    const int key[7] = {G.B, G.Hkv, G.g, G.Dh, A, kv_len, fc_knobs().version + 1};
+    for (const Entry &e : known)
+        if (e.cap == cap && !memcmp(e.key, key, sizeof key)) return e.plan;
+    Entry &e = known[next++ % 4];
+    memcpy(e.key, key, sizeof key);
+    e.cap = cap;
+    return e.plan = plan(G, A, kv_len, cap);
 }
 
 hipError_t fc_launch_q4_attention(const FcQ4Geom &G, const FcQ4Plan &pl, const void *q, const uint8_t *layer, const int32_t *pos, const int32_t *lens,
