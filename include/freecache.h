@@ -420,8 +420,8 @@ fc_status fc_gather_rows(int32_t dtype, const void *table, int32_t rows, int32_t
  * and with W the sum of w over the shortest of the prefixes
  *   tok[m] = the first entry of the order at which the running sum of w exceeds u[m] W,   conf[m] = w[tok[m]] / W.
  * temperature 0 is the arg-max with conf = softmax(z)[tok] as in fc_lm_head_argmax; top_k, top_p, min_p and u are then not looked at.
- * Sums are whole numbers, the largest w being 2^(62 - ceil(log2 V)), at most 2^52: the same bits from call to call, whatever else is in the batch,
- * and w below half a unit (2^-45 at 152064 entries) count as 0.  NaN entries are passed over, -inf ones have w = 0; of several +inf each has w = 1 and
+ * A row gives the same bits from call to call and whatever else is in the batch.  Weights are exact to 2^-33 of themselves; entries 32 temperatures and more
+ * below the largest (w < 1.3e-14) count as w = 0.  NaN entries are passed over, -inf ones have w = 0; of several +inf each has w = 1 and
  * the finite ones 0.  A row of nothing but NaN and -inf gets tok = -1, conf = 0.
  */
 
@@ -432,7 +432,7 @@ size_t fc_sample_workspace_bytes(int32_t dtype, int32_t M, int32_t V);
  *   u       device float [M], uniform in [0, 1); below 0 counts as 0, 1 or more (and NaN) picks the last kept entry.  May be NULL at temperature 0.
  *   tok  device int32 [M];  conf  device float [M];  workspace  device, 16-byte aligned, >= fc_sample_workspace_bytes(dtype, M, V) bytes
  * Errors: INVALID_ARG (NULL; M, V < 1; ld < V; temperature < 0 or not finite; top_k < 0; top_p outside (0, 1]; min_p outside [0, 1]),
- * UNSUPPORTED (V or M beyond 2^24), WORKSPACE, HIP. */
+ * UNSUPPORTED (V beyond 2^24, M beyond 65535), WORKSPACE, HIP. */
 fc_status fc_sample_tokens(int32_t dtype, const void *logits, int64_t ld, int32_t M, int32_t V, float temperature, int32_t top_k,
                            float top_p, float min_p, const float *u, int32_t *tok, float *conf, void *workspace,
                            size_t workspace_bytes, void *stream);

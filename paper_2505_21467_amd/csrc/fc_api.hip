@@ -1574,7 +1574,7 @@ fc_status fc_q4_attention(const fc_q4_cache *cache, int32_t layer, const void *q
 
 size_t fc_sample_workspace_bytes(int32_t dtype, int32_t M, int32_t V)
 {
-    if ((dtype != FC_F32 && dtype != FC_BF16) || M < 1 || V < 1 || M > (1 << 24) || V > (1 << 24)) return 0;
+    if ((dtype != FC_F32 && dtype != FC_BF16) || M < 1 || V < 1 || M > 65535 || V > (1 << 24)) return 0;
     return fc_sample_workspace(dtype, M, V);
 }
 
@@ -1594,7 +1594,7 @@ fc_status fc_sample_tokens(int32_t dtype, const void *logits, int64_t ld, int32_
         if (!(top_p > 0.f && top_p <= 1.f)) return fail(FC_ERR_INVALID_ARG, "top_p must be in (0, 1]");
         if (!(min_p >= 0.f && min_p <= 1.f)) return fail(FC_ERR_INVALID_ARG, "min_p must be in [0, 1]");
     }
-    if (M > (1 << 24) || V > (1 << 24)) return fail(FC_ERR_UNSUPPORTED, "M and V are limited to 2^24");
+    if (M > 65535 || V > (1 << 24)) return fail(FC_ERR_UNSUPPORTED, "M is limited to 65535, V to 2^24");
     if ((uintptr_t)workspace & 15) return fail(FC_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
     const size_t need = fc_sample_workspace(dtype, M, V), given = workspace ? workspace_bytes : 0;
     if (given < need) return fail(FC_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, given);
@@ -1607,9 +1607,6 @@ fc_status fc_sample_tokens(int32_t dtype, const void *logits, int64_t ld, int32_
     p.top_p = greedy ? 1.f : top_p;
     p.min_p = greedy ? 0.f : min_p;
     p.inv_t = greedy ? 1.0 : 1.0 / (double)temperature;
-    int bits = 62;
-    while (bits > 38 && ((int64_t)1 << (62 - bits)) < V) --bits;
-    p.one = ldexp(1.0, bits < 52 ? bits : 52);  // (whole in fp64)
     p.greedy = greedy;
     p.u = u;
     p.tok = tok;

@@ -9,7 +9,7 @@ struct FcSampleArgs {
     int64_t ld;  // elements from row to row
     int32_t M, V, top_k;
     float top_p, min_p;
-    double inv_t, one;  // 1 / temperature; the whole number that stands for the largest weight
+    double inv_t;  // 1 / temperature (1 where that is 0)
     int32_t greedy;
     const float *u;
     int32_t *tok;

@@ -34,8 +34,8 @@ def _check(z, dtype, u, V=None, offset=0, what="", **k):
         p = {**dict(temperature=1.0, top_k=0, top_p=1.0, min_p=0.0), **k}
         t, c = ref.sample(z[m, :V].numpy(), u=0.0 if u is None else float(u[m]), **p)
         assert tok[m] == t, "%s row %d: token %d, %d by definition" % (what, m, tok[m], t)
-        # weights to half a unit of 2^-(62 - log2 V) of the largest, V of them; one rounding to fp32
-        assert abs(conf[m] - c) <= 2.0 ** -24 * c + z.shape[1] * 2.0 ** -44, "%s row %d: confidence %r, %r" % (what, m, conf[m], c)
+        # weights and sums to 2^-33 of themselves, less than 2^-44 of each entry lost; one rounding to fp32
+        assert abs(float(conf[m]) - c) <= 2.0 ** -24 * c + z.shape[1] * 2.0 ** -44, "%s row %d: confidence %r, %r" % (what, m, conf[m], c)
 
 
 def _logits(seed, M, V, spread, peaks=14.0):
