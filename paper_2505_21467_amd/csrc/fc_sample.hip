@@ -22,103 +22,166 @@
 namespace {
 
 constexpr int BINS = 1024, PER_T = 32;       // bins; bins to a unit of z / T
-constexpr int SCAN = 512, VPT = 32;          // threads and values per thread of a part
-constexpr int PART = SCAN * VPT;             // entries of a part: its counts fit 15 bits, its sums 47
+constexpr int SCAN = 512, PART = 16384;      // threads, and entries of a part: its counts fit 15 bits, its sums 47
 constexpr int PICK = 1024;                   // threads of the second kernel, one to a bin
-constexpr int CAP = 10240;                   // entries that it fetches into LDS
-constexpr uint64_t SUM_BITS = 48;
+constexpr int CAP = 5120;                    // entries that it fetches into LDS
+constexpr int FEW = 32;                      // entries that one wave compares with one another
+constexpr int SUM_BITS = 48;
 
 __host__ __device__ inline int parts_of(int V) { return (V + PART - 1) / PART; }
 
-// Order-preserving image of a logit.  -0 is 0.
-__device__ __forceinline__ uint32_t key_of(float z)
+// Order of the entries as a number: the larger logit first, then the smaller index.  -0 is 0.
+__device__ __forceinline__ uint64_t rank_of(float z, uint32_t index)
 {
     const uint32_t u = __float_as_uint(z + 0.f);
-    return u & 0x80000000u ? ~u : u | 0x80000000u;
+    return (uint64_t)(u & 0x80000000u ? ~u : u | 0x80000000u) << 32 | (uint32_t)~index;
 }
-__device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
+__device__ __forceinline__ float logit_of(uint64_t rank)
+{
+    const uint32_t key = (uint32_t)(rank >> 32);
+    return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
+}
 
-// Bin of a finite logit on the grid, and where it lies in it (0 .. 1 from the lower edge).
-struct Place {
-    double bin, within;
-    __device__ __forceinline__ Place(float z, double c)
+// The grid as seen from a largest logit: in which bin below its own a logit is, BINS or more if in none, and its weight over the upper edge's.
+struct Grid {
+    float most;
+    bool infinite;  // then the infinite logits are in bin 0, and no others in any
+    double c, top;  // bins to a unit of logit; the largest logit's bin
+    __device__ __forceinline__ Grid(float most_, double c_) : most(most_), infinite(most_ > 3.4028235e38f), c(c_), top(floor((double)most_ * c_)) {}
+    __device__ __forceinline__ int bin(float z, double &within) const
     {
-        const double x = (double)z * c;
-        bin = floor(x);
-        within = x - bin;
+        const double x = (double)z * c, b = floor(x);
+        within = x - b;
+        const double d = top - b;
+        if (infinite) return z == most ? 0 : BINS;
+        return d < (double)BINS ? (int)d : BINS;  // (NaN: none)
     }
     // exp((within - 1) / 32) in units of 2^-32: a Taylor series about the middle of the bin, off by less than 2^-45.
-    __device__ __forceinline__ uint64_t weight() const
+    __device__ __forceinline__ uint64_t weight(double within) const
     {
+        if (infinite) return 1ull << 32;
         const double u = (within - 0.5) * (1.0 / PER_T);
         const double e = 1.0 + u * (1.0 + u * (1.0 / 2 + u * (1.0 / 6 + u * (1.0 / 24 + u * (1.0 / 120)))));
-        return (uint64_t)__double_as_longlong(e * 0.98449643700540845 * 4294967296.0 + 4503599627370496.0) & 0xfffffffffffffull;  // exp(-1/64); 2^52 rounds
+        return (uint64_t)__double_as_longlong(e * (0.98449643700540845 * 4294967296.0) + 4503599627370496.0) & 0xfffffffffffffull;  // exp(-1/64); 2^52 rounds
+    }
+    // Logits of bins b0 .. b1, and perhaps a few more on either side.
+    __device__ __forceinline__ float lowest(int b1) const
+    {
+        const float x = (float)((top - b1) / c);
+        return infinite ? most : x - fabsf(x) * 3e-7f;
+    }
+    __device__ __forceinline__ float highest(int b0) const
+    {
+        const float x = (float)((top - b0 + 1.) / c);
+        return infinite ? most : x + fabsf(x) * 3e-7f;
     }
 };
-// Distance in bins from the one of the largest entry; BINS or more: not in any.  Infinite logits: the largest are in bin 0, at its upper edge.
-__device__ __forceinline__ bool in_bins(float z, float z_max, double top, double c, int &bin, uint64_t &w)
+
+// Entries of a row's piece of n, 16 bytes of a thread at a time: f(first index, values), -inf beyond the end.
+template <typename T, int THREADS, typename F>
+__device__ __forceinline__ void each_piece(const T *z, int n, F f)
 {
-    if (z == z_max && z > 3.4028235e38f) {
-        bin = 0;
-        w = 1ull << 32;
-        return true;
+    constexpr int N = 16 / sizeof(T);
+    struct Piece { T v[N]; };
+#pragma unroll 1
+    for (int i0 = threadIdx.x * N; i0 < n; i0 += 2 * THREADS * N) {
+        Piece x[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            const int at = i0 + k * THREADS * N;
+            if (at + N <= n) x[k] = __builtin_bit_cast(Piece, fc_load_any<uint4>(z + at));
+            else
+                for (int j = 0; j < N; ++j) x[k].v[j] = at + j < n ? z[at + j] : fc_from_float<T>(-__builtin_inff());
+        }
+#pragma unroll 1
+        for (int k = 0; k < 2; ++k) {
+            float v[N];
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[j] = fc_to_float(k ? x[1].v[j] : x[0].v[j]);
+            f(i0 + k * THREADS * N, v);
+        }
     }
-    const Place p(z, c);
-    const double d = top - p.bin;
-    if (!(d < (double)BINS)) return false;  // (NaN, and everything below infinity, too)
-    bin = (int)d;
-    w = p.weight();
-    return true;
 }
 
-template <typename T>
-struct Piece {
-    static constexpr int N = 16 / sizeof(T);
-    T v[N];
-};
+// Inclusive running sum over a wave.
+template <typename X>
+__device__ __forceinline__ X wave_scan(X x)
+{
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const X y = __shfl_up(x, o);
+        if ((threadIdx.x & 63) >= (unsigned)o) x += y;
+    }
+    return x;
+}
 
-// One part of a row: bins[] gets (entries << 48 | sum of weights).
-template <typename T>
+// One part of a row: bins[] gets (entries << 48 | sum of weights).  With a top-k nothing below the part's own k-th entry can be kept, so its entries
+// are counted first and only those weighed: a count takes half the time of a weight and its sum (256 rows x 152064: see the figures at the launch).
+template <typename T, bool TOP_K>
 __global__ __launch_bounds__(SCAN) void k_sample_bins(FcSampleArgs p, int parts, uint64_t *__restrict__ bins, float *__restrict__ largest)
 {
-    constexpr int N = Piece<T>::N, PIECES = VPT / N;
-    __shared__ uint64_t s_bin[BINS];
+    constexpr int N = 16 / sizeof(T);
+    __shared__ unsigned long long s_bin[BINS];
+    __shared__ uint32_t s_count[TOP_K ? BINS : 1], s_wave[SCAN / 64];
     __shared__ float s_max[SCAN / 64];
-    const int tid = threadIdx.x, part = blockIdx.x, row = blockIdx.y;
+    __shared__ int s_last;
+    const int tid = threadIdx.x;
+    const uint32_t row = blockIdx.x / (uint32_t)parts, part = blockIdx.x - row * parts;
     const int from = part * PART, n = min(p.V - from, PART);
     const T *z = (const T *)p.logits + (size_t)row * p.ld + from;
-    Piece<T> x[PIECES];
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-        const int at = (i * SCAN + tid) * N;
-        if (at + N <= n) x[i] = __builtin_bit_cast(Piece<T>, fc_load_any<uint4>(z + at));
-        else
-#pragma unroll
-            for (int j = 0; j < N; ++j) x[i].v[j] = at + j < n ? z[at + j] : fc_from_float<T>(-__builtin_inff());
-    }
-#pragma unroll
-    for (int i = tid; i < BINS; i += SCAN) s_bin[i] = 0;
     float top = -__builtin_inff();
+    each_piece<T, SCAN>(z, n, [&](int, const float(&v)[N]) {
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i)
-#pragma unroll
-        for (int j = 0; j < N; ++j) top = fmaxf(top, fc_to_float(x[i].v[j]));  // (NaN is passed over)
+        for (int j = 0; j < N; ++j) top = fmaxf(top, v[j]);  // (NaN is passed over)
+    });
+    for (int i = tid; i < BINS; i += SCAN) {
+        s_bin[i] = 0;
+        if (TOP_K) s_count[i] = 0;
+    }
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
     if (tid % 64 == 0) s_max[tid / 64] = top;
+    if (tid == 0) s_last = BINS - 1;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < SCAN / 64; ++i) top = fmaxf(top, s_max[i]);
-    const double c = p.inv_t * PER_T, base = floor((double)top * c);
     if (top > -__builtin_inff()) {
+        const Grid g(top, p.inv_t * PER_T);
+        int last = min(p.last_bin, BINS - 1);
+        if constexpr (TOP_K) {
+            const float cut = g.lowest(last);
+            each_piece<T, SCAN>(z, n, [&](int, const float(&v)[N]) {
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i)
+                for (int j = 0; j < N; ++j) {
+                    double within;
+                    if (v[j] >= cut) {
+                        const int b = g.bin(v[j], within);
+                        if (b < BINS) atomicAdd(&s_count[b], 1u);
+                    }
+                }
+            });
+            __syncthreads();
+            const uint32_t a = s_count[2 * tid], b = s_count[2 * tid + 1];
+            uint32_t run = wave_scan(a + b);
+            if (tid % 64 == 63) s_wave[tid / 64] = run;
+            __syncthreads();
+            for (int i = 0; i < tid / 64; ++i) run += s_wave[i];
+            const uint32_t k = (uint32_t)p.top_k, first = run - b;
+            if (run >= k && run - a - b < k) s_last = first >= k ? 2 * tid : 2 * tid + 1;
+            __syncthreads();
+            last = min(last, s_last);
+        }
+        const float cut = g.lowest(last);
+        each_piece<T, SCAN>(z, n, [&](int, const float(&v)[N]) {
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                int bin;
-                uint64_t w;
-                if (in_bins(fc_to_float(x[i].v[j]), top, base, c, bin, w)) atomicAdd((unsigned long long *)&s_bin[bin], (unsigned long long)(1ull << SUM_BITS | w));
+                double within;
+                if (v[j] >= cut) {
+                    const int b = g.bin(v[j], within);
+                    if (b <= last) atomicAdd(&s_bin[b], (unsigned long long)(1ull << SUM_BITS | g.weight(within)));
+                }
             }
+        });
     }
     __syncthreads();
     const size_t at = (size_t)row * parts + part;
@@ -126,136 +189,179 @@ __global__ __launch_bounds__(SCAN) void k_sample_bins(FcSampleArgs p, int parts,
     if (tid == 0) largest[at] = top;
 }
 
+struct Entry {
+    uint64_t rank, bin_weight;  // bin << 40 | weight
+};
+
 struct PickShared {
-    double cum[BINS];       // running sums of weights over the bins, from the largest logit down
+    double cum[BINS];       // running sums of weights over the bins, from the largest logit down, in units of 2^-32 of bin 0's upper edge
+    double factor[BINS];    // exp(-bin / 32)
     uint32_t count[BINS];   // running counts
-    uint64_t sum[BINS];     // the bins' sums, in units of 2^-32 of their upper edge's weight
-    uint32_t key[CAP], index[CAP];
-    uint16_t bin[CAP];
+    uint64_t sum[BINS];     // the bins' own sums
+    Entry list[CAP];
     uint8_t marked[BINS];
     double wave_sum[PICK / 64];
     uint32_t wave_count[PICK / 64];
     uint64_t digit_sum[256];
     uint32_t digit_count[256];
-    uint32_t n, low, high, found[2];
-    uint64_t found_sum;
-    int first;
+    Entry few[FEW];
+    unsigned long long low, high, sum_found, rank_found, weight_found;
+    uint32_t n, digit, count_found;
 };
-
-// Thread i's `x`: the first i for which it holds, BINS if for none.
-__device__ int first_bin(PickShared &s, bool x)
-{
-    __syncthreads();
-    if (threadIdx.x == 0) s.first = BINS;
-    __syncthreads();
-    const uint64_t b = __ballot(x);
-    if (b && threadIdx.x % 64 == 0) atomicMin(&s.first, (int)threadIdx.x + __builtin_ctzll(b));
-    __syncthreads();
-    return s.first;
-}
 
 struct Found {
-    uint32_t key, count, ties;  // entries with larger keys, and with this one
-    uint64_t sum;               // weight of those with larger keys
+    uint64_t rank, sum, weight;  // the entry, the weight of all up to it, its own
 };
 
-// Among the entries that each(f) calls f(key, weight) for: the key of the one at which the running count (COUNT) or sum, larger keys first, passes
-// `target`.  Digits of 8 bits, from the first bit in which the keys differ.
+// Among the n entries that each(f) calls f(rank, weight) for: the one at which the running count (COUNT) or sum, larger ranks first, passes
+// `target`; the last one if none does.  Digits of 8 bits from the first bit in which the ranks differ, until a wave can compare what is left.
 template <bool COUNT, typename EACH>
-__device__ Found descend(PickShared &s, uint64_t target, EACH each)
+__device__ Found select(PickShared &s, uint32_t n, uint64_t target, EACH each)
 {
     const int tid = threadIdx.x;
-    __syncthreads();
-    if (tid == 0) {
-        s.low = 0xffffffffu;
-        s.high = 0;
-    }
-    __syncthreads();
-    uint32_t low = 0xffffffffu, high = 0;
-    each([&](uint32_t key, uint64_t) {
-        low = min(low, key);
-        high = max(high, key);
-    });
-    for (int o = 1; o < 64; o <<= 1) {
-        low = min(low, (uint32_t)__shfl_xor((int)low, o));
-        high = max(high, (uint32_t)__shfl_xor((int)high, o));
-    }
-    if (tid % 64 == 0 && low <= high) {
-        atomicMin(&s.low, low);
-        atomicMax(&s.high, high);
-    }
-    __syncthreads();
-    int pos = s.low == s.high ? 1 : 32 - __builtin_clz(s.low ^ s.high);  // (one digit of one bit where all are equal)
-    Found f{s.high, 0, 0, 0};
-    while (pos > 0) {
-        const int bits = min(pos, 8), shift = pos - bits;
+    uint64_t low = 0, high = ~0ull, sum = 0;
+    uint32_t count = 0;
+#pragma unroll 1
+    while (n > FEW) {
         __syncthreads();
+        if (tid == 0) {
+            s.low = ~0ull;
+            s.high = 0;
+        }
         if (tid < 256) {
             s.digit_sum[tid] = 0;
             s.digit_count[tid] = 0;
         }
         __syncthreads();
-        each([&](uint32_t key, uint64_t w) {
-            if (pos < 32 && (key ^ f.key) >> pos) return;
-            const uint32_t d = key >> shift & ((1u << bits) - 1);
+        uint64_t a = ~0ull, b = 0;
+        each([&](uint64_t rank, uint64_t) {
+            if (rank < low || rank > high) return;
+            a = min(a, rank);
+            b = max(b, rank);
+        });
+        if (a <= b) {
+            atomicMin(&s.low, (unsigned long long)a);
+            atomicMax(&s.high, (unsigned long long)b);
+        }
+        __syncthreads();
+        const int bits = 64 - __builtin_clzll(s.low ^ s.high), shift = bits > 8 ? bits - 8 : 0;
+        const uint32_t mask = (uint32_t)((bits - shift < 8 ? 1u << (bits - shift) : 256u) - 1);
+        each([&](uint64_t rank, uint64_t w) {
+            if (rank < low || rank > high) return;
+            const uint32_t d = (uint32_t)(rank >> shift) & mask;
             atomicAdd((unsigned long long *)&s.digit_sum[d], (unsigned long long)w);
             atomicAdd(&s.digit_count[d], 1u);
         });
         __syncthreads();
         if (tid < 64) {  // lane i has the digits 255 - 4 i .. 252 - 4 i
-            uint64_t sum = 0;
-            uint32_t count = 0;
+            unsigned long long own = 0;
+            uint32_t owns = 0;
             for (int i = 0; i < 4; ++i) {
-                sum += s.digit_sum[255 - 4 * tid - i];
-                count += s.digit_count[255 - 4 * tid - i];
+                own += s.digit_sum[255 - 4 * tid - i];
+                owns += s.digit_count[255 - 4 * tid - i];
             }
-            uint64_t run = sum;
-            uint32_t runs = count;
-            for (int o = 1; o < 64; o <<= 1) {
-                const uint64_t x = (uint64_t)__shfl_up((unsigned long long)run, o);
-                const uint32_t y = (uint32_t)__shfl_up((int)runs, o);
-                if (tid >= o) {
-                    run += x;
-                    runs += y;
-                }
-            }
-            const uint64_t passed = __ballot(COUNT ? f.count + runs > target : f.sum + run > target);
-            const int lane = passed ? __builtin_ctzll(passed) : 63;
+            unsigned long long run = sum + wave_scan(own);
+            uint32_t runs = count + wave_scan(owns);
+            const uint64_t passed = __ballot(COUNT ? runs > target : run > target), some = __ballot(owns > 0);
+            const int lane = passed ? __builtin_ctzll(passed) : 63 - __builtin_clzll(some);  // (none: the last one with entries)
             if (tid == lane) {
-                run += f.sum - sum;
-                runs += f.count - count;
-                int d = 255 - 4 * tid;
-                for (int i = 0; i < 3; ++i, --d) {
+                run -= own;
+                runs -= owns;
+                int d = 255 - 4 * tid, last = d;
+                for (int i = 0; i < 4; ++i, --d) {
+                    if (!s.digit_count[d]) continue;
+                    last = d;
                     if (COUNT ? runs + s.digit_count[d] > target : run + s.digit_sum[d] > target) break;
                     run += s.digit_sum[d];
                     runs += s.digit_count[d];
                 }
-                s.found[0] = (uint32_t)d;
-                s.found[1] = runs;
-                s.found_sum = run;
+                if (d < 255 - 4 * tid - 3) {  // none passes: the last digit that has entries
+                    run -= s.digit_sum[last];
+                    runs -= s.digit_count[last];
+                }
+                s.digit = (uint32_t)last;
+                s.sum_found = run;
+                s.count_found = runs;
             }
         }
         __syncthreads();
-        f.key = (pos < 32 ? f.key >> pos << pos : 0) | s.found[0] << shift;
-        f.count = s.found[1];
-        f.sum = s.found_sum;
-        f.ties = s.digit_count[s.found[0]];
-        pos = shift;
+        sum = s.sum_found;
+        count = s.count_found;
+        n = s.digit_count[s.digit];
+        low = (bits < 64 ? s.low >> bits << bits : 0) | (uint64_t)s.digit << shift;
+        high = low | ((1ull << shift) - 1);
     }
-    return f;
+    __syncthreads();
+    if (tid == 0) s.n = 0;
+    __syncthreads();
+    each([&](uint64_t rank, uint64_t w) {
+        if (rank < low || rank > high) return;
+        const uint32_t at = atomicAdd(&s.n, 1u);
+        if (at < FEW) s.few[at] = Entry{rank, w};
+    });
+    __syncthreads();
+    n = min(s.n, (uint32_t)FEW);
+    if (tid < (int)n) {
+        const Entry own = s.few[tid];
+        uint64_t run = sum;
+        uint32_t runs = 0;
+        for (uint32_t i = 0; i < n; ++i)
+            if (s.few[i].rank > own.rank) {
+                run += s.few[i].bin_weight;
+                ++runs;
+            }
+        const bool passes = COUNT ? count + runs + 1 > target : run + own.bin_weight > target;
+        const bool before = COUNT ? count + runs > target : run > target;
+        if ((passes && !before) || (!passes && runs == n - 1)) {
+            s.rank_found = own.rank;
+            s.sum_found = run + own.bin_weight;
+            s.weight_found = own.bin_weight;
+        }
+    }
+    __syncthreads();
+    return Found{s.rank_found, s.sum_found, s.weight_found};
+}
+
+// The entries of bin b: those of the list, or (LIST false) found in the row once more.
+template <typename T, bool LIST, bool COUNT>
+__device__ __attribute__((noinline)) Found select_in(PickShared &s, const T *z, int V, const Grid &g, int listed, int b, uint32_t n, uint64_t target)
+{
+    if constexpr (LIST) {
+        return select<COUNT>(s, n, target, [&](auto f) {
+            for (int i = threadIdx.x; i < listed; i += PICK) {
+                const Entry e = s.list[i];
+                if ((int)(e.bin_weight >> 40) == b) f(e.rank, e.bin_weight & ((1ull << 40) - 1));
+            }
+        });
+    } else {
+        const float low = g.lowest(b), high = g.highest(b);
+        constexpr int N = 16 / sizeof(T);
+        return select<COUNT>(s, n, target, [&](auto f) {
+            each_piece<T, PICK>(z, V, [&](int at, const float(&v)[N]) {
+#pragma unroll 1
+                for (int j = 0; j < N; ++j) {
+                    double within;
+                    if (v[j] >= low && v[j] <= high && g.bin(v[j], within) == b) f(rank_of(v[j], (uint32_t)(at + j)), g.weight(within));
+                }
+            });
+        });
+    }
 }
 
 template <typename T>
 __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts, const uint64_t *__restrict__ bins, const float *__restrict__ largest)
 {
     __shared__ PickShared s;
-    constexpr int N = Piece<T>::N;
+    constexpr int N = 16 / sizeof(T);
     const int tid = threadIdx.x, row = blockIdx.x;
     const T *z = (const T *)p.logits + (size_t)row * p.ld;
-    const double c = p.inv_t * PER_T;
+    const float *most = largest + (size_t)row * parts;
+    const uint64_t *part = bins + (size_t)row * parts * BINS;
 
     float z_max = -__builtin_inff();
-    for (int i = 0; i < parts; ++i) z_max = fmaxf(z_max, largest[(size_t)row * parts + i]);
+    for (int i = tid % 64; i < parts; i += 64) z_max = fmaxf(z_max, most[i]);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) z_max = fmaxf(z_max, __shfl_xor(z_max, o));
     if (z_max == -__builtin_inff()) {
         if (tid == 0) {
             p.tok[row] = -1;
@@ -263,219 +369,181 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
         }
         return;
     }
-    const bool infinite = z_max > 3.4028235e38f;
-    const double top = floor((double)z_max * c);
+    const Grid g(z_max, p.inv_t * PER_T);
 
     // Thread i: bin i of the row.
     uint32_t count = 0;
     uint64_t sum = 0;
 #pragma unroll 4
     for (int i = 0; i < parts; ++i) {
-        const float m = largest[(size_t)row * parts + i];
-        const double off = infinite ? (m == z_max ? 0. : (double)BINS) : top - floor((double)m * c);  // (a part of nothing is infinitely far)
-        const int at = off < (double)BINS ? tid - (int)off : -1;
-        const uint64_t x = at >= 0 ? bins[((size_t)row * parts + i) * BINS + at] : 0;
-        count += (uint32_t)(x >> SUM_BITS);
-        sum += x & ((1ull << SUM_BITS) - 1);
+        double within;
+        const int at = tid - g.bin(most[i], within);  // (a part of nothing is in no bin)
+        const uint64_t x = part[(size_t)i * BINS + max(at, 0)];
+        count += at >= 0 ? (uint32_t)(x >> SUM_BITS) : 0;
+        sum += at >= 0 ? x & ((1ull << SUM_BITS) - 1) : 0;
     }
     const double factor = exp(-(double)tid / PER_T);
-    double cum = (double)sum * factor;
-    uint32_t counts = count;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const double x = __shfl_up(cum, o);
-        const uint32_t y = (uint32_t)__shfl_up((int)counts, o);
-        if (tid % 64 >= o) {
-            cum += x;
-            counts += y;
-        }
-    }
+    double cum = wave_scan((double)sum * factor);
+    uint32_t counts = wave_scan(count);
     if (tid % 64 == 63) {
         s.wave_sum[tid / 64] = cum;
         s.wave_count[tid / 64] = counts;
     }
     s.sum[tid] = sum;
+    s.factor[tid] = factor;
     s.marked[tid] = 0;
     if (tid == 0) s.n = 0;
     __syncthreads();
-    {
-        double x = 0.;
-        uint32_t y = 0;
-        for (int i = 0; i < tid / 64; ++i) {
-            x += s.wave_sum[i];
-            y += s.wave_count[i];
-        }
-        cum += x;
-        counts += y;
+    for (int i = 0; i < tid / 64; ++i) {
+        cum += s.wave_sum[i];
+        counts += s.wave_count[i];
     }
     s.cum[tid] = cum;
     s.count[tid] = counts;
     __syncthreads();
-    const double all = s.cum[BINS - 1];
+
     auto before = [&](int b) { return b > 0 ? s.cum[b - 1] : 0.; };
     auto counted = [&](int b) { return b > 0 ? s.count[b - 1] : 0u; };
-    const double u = p.greedy ? 0. : (double)p.u[row];
+    // The first bin whose running sum reaches x, or (past) exceeds it; BINS if none does.
+    auto reach = [&](double x, bool past) {
+        int b = 0;
+#pragma unroll 1
+        for (int step = BINS / 2; step; step >>= 1)
+            if (past ? s.cum[b + step - 1] <= x : s.cum[b + step - 1] < x) b += step;
+        return (past ? s.cum[b] <= x : s.cum[b] < x) ? BINS : b;
+    };
+    const double all = s.cum[BINS - 1], u = p.greedy ? 0. : (double)p.u[row];
+    const bool inside = u < 1.;  // (NaN: not)
+    // The bin of the token for this total of kept weights: where u times it is exceeded, or the last kept entry's.
+    auto token_bin = [&](double total) {
+        const int b = inside ? reach(fmax(u, 0.) * total, true) : reach(total, false);
+        return b < BINS ? b : reach(all, false);
+    };
 
     // Where the targets can lie: the total is known but for the bins in which filters end.
     double low = all, high = all;
     int kb = BINS, mb = BINS, pb0 = BINS, pb1 = -1;
-    if (p.top_k > 0) {
-        kb = first_bin(s, counts >= (uint32_t)p.top_k);  // (none: what is kept beyond the bins weighs nothing)
-        if (kb < BINS) {
-            low = before(kb);
-            high = s.cum[kb];
-        }
+    if (p.top_k > 0 && s.count[BINS - 1] >= (uint32_t)p.top_k) {  // (otherwise what is kept beyond the bins weighs nothing)
+        kb = 0;
+#pragma unroll 1
+        for (int step = BINS / 2; step; step >>= 1)
+            if (s.count[kb + step - 1] < (uint32_t)p.top_k) kb += step;
+        low = before(kb);
+        high = s.cum[kb];
     }
     if (p.top_p < 1.f) {
-        pb0 = min(first_bin(s, cum >= (double)p.top_p * low), BINS - 1);
-        pb1 = kb < BINS ? min(first_bin(s, cum >= (double)p.top_p * high), BINS - 1) : pb0;
+        pb0 = min(reach((double)p.top_p * low, false), BINS - 1);
+        pb1 = kb < BINS ? min(reach((double)p.top_p * high, false), BINS - 1) : pb0;
         low = fmin(low, before(pb0));
         high = fmin(high, s.cum[pb1]);
     }
-    if (p.min_p > 0.f && !infinite) {
-        const double d = top - floor((double)z_max * c + log((double)p.min_p) * PER_T);
-        if (d < (double)BINS) {
+    if (p.min_p > 0.f && !g.infinite) {
+        const double d = g.top - floor((double)z_max * g.c + p.log_min_p * PER_T);
+        if (d <= (double)min(kb, BINS - 1)) {  // (beyond the bin in which top-k ends it keeps more)
             mb = (int)d;
             low = fmin(low, before(mb));
             high = fmin(high, s.cum[mb]);
         }
     }
-    // The bin in which u times the total lies: the first whose running sum exceeds it, and one with entries.
-    auto target_bin = [&](double total) {
-        const int b = u < 1. ? first_bin(s, cum > (u > 0. ? u : 0.) * total) : BINS;  // (NaN: none)
-        return b < BINS ? b : first_bin(s, cum >= all);
-    };
-    auto last_bin = [&](double total) { return min(first_bin(s, cum >= total), BINS - 1); };
-    const bool inside = u < 1.;
-    int sb0 = inside ? target_bin(low) : last_bin(low), sb1 = inside ? (low < high ? target_bin(high) : sb0) : last_bin(high);
-    const bool mark = tid == kb || tid == mb || (tid >= pb0 && tid <= pb1) || (tid >= sb0 && tid <= sb1);
+    const int sb0 = token_bin(low), sb1 = low < high ? token_bin(high) : sb0;
+    const bool filter = tid == kb || tid == mb || (tid >= pb0 && tid <= pb1), mark = filter || (tid >= sb0 && tid <= sb1);
     s.marked[tid] = mark;
-    if (mark) atomicAdd(&s.n, count);
+    if (mark && count) atomicAdd(&s.n, count);
+    // Logits of the filters' bins, and of the token's.
+    const int f0 = min(min(kb, mb), pb0), f1 = max(max(kb < BINS ? kb : -1, mb < BINS ? mb : -1), pb1);
+    const float flow = f1 < 0 ? __builtin_inff() : g.lowest(f1), fhigh = f1 < 0 ? -__builtin_inff() : g.highest(f0);
+    const float slow = g.lowest(sb1), shigh = g.highest(sb0);
     __syncthreads();
-    const int marked = (int)s.n;
-    const bool listed = marked <= CAP;
+    const bool list = s.n <= (uint32_t)CAP;
     __syncthreads();
     if (tid == 0) s.n = 0;
-    // No entry below this logit is in a marked bin (a bin to spare for the rounding).
-    const int deepest = max(max(sb1, pb1), max(kb < BINS ? kb : 0, mb < BINS ? mb : 0));
-    const float lowest = (float)((top - deepest - 1.) / c), cut = infinite ? z_max : lowest - fabsf(lowest) * 1e-6f;
     __syncthreads();
-
-    // Every entry of the row in a bin: f(index, logit, bin, weight).
-    auto scan = [&](auto f) {
-        for (int i0 = tid * N; i0 < p.V; i0 += PICK * N * 4) {
-            Piece<T> x[4];
+    if (list) {
+        each_piece<T, PICK>(z, p.V, [&](int at, const float(&v)[N]) {
+            uint32_t hit = 0;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int at = i0 + k * PICK * N;
-                if (at + N <= p.V) x[k] = __builtin_bit_cast(Piece<T>, fc_load_any<uint4>(z + at));
-                else
+            for (int j = 0; j < N; ++j) hit |= ((v[j] >= slow && v[j] <= shigh) || (v[j] >= flow && v[j] <= fhigh) ? 1u : 0u) << j;
+            while (hit) {
+                const int j = __builtin_ctz(hit);
+                hit &= hit - 1;
+                float x = v[0];
 #pragma unroll
-                    for (int j = 0; j < N; ++j) x[k].v[j] = at + j < p.V ? z[at + j] : fc_from_float<T>(-__builtin_inff());
+                for (int i = 1; i < N; ++i) x = j == i ? v[i] : x;
+                double within;
+                const int b = g.bin(x, within);
+                if (b >= BINS || !s.marked[b]) continue;
+                const uint32_t to = atomicAdd(&s.n, 1u);
+                if (to < CAP) s.list[to] = Entry{rank_of(x, (uint32_t)(at + j)), (uint64_t)b << 40 | g.weight(within)};
             }
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-#pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    const float v = fc_to_float(x[k].v[j]);
-                    int bin;
-                    uint64_t w;
-                    if (v >= cut && in_bins(v, z_max, top, c, bin, w)) f(i0 + k * PICK * N + j, v, bin, w);
-                }
-        }
-    };
-    if (listed) {
-        scan([&](int i, float v, int bin, uint64_t) {
-            if (!s.marked[bin]) return;
-            const uint32_t at = atomicAdd(&s.n, 1u);
-            s.key[at] = key_of(v);
-            s.index[at] = (uint32_t)i;
-            s.bin[at] = (uint16_t)bin;
         });
         __syncthreads();
     }
-    const int n = listed ? (int)s.n : 0;
-    auto weight = [&](float v) {
-        int bin;
-        uint64_t w = 0;
-        in_bins(v, z_max, top, c, bin, w);
-        return w;
-    };
-    // The entries of one bin: f(key, index, weight).
-    auto entries = [&](int b, auto f) {
-        if (listed) {
-            for (int i = tid; i < n; i += PICK)
-                if (s.bin[i] == b) f(s.key[i], s.index[i], weight(logit_of(s.key[i])));
-        } else {
-            scan([&](int i, float v, int bin, uint64_t w) {
-                if (bin == b) f(key_of(v), (uint32_t)i, w);
-            });
-        }
-    };
-    auto select = [&](auto counting, int b, uint64_t target) {
-        return descend<decltype(counting)::value>(s, target, [&](auto f) { entries(b, [&](uint32_t key, uint32_t, uint64_t w) { f(key, w); }); });
-    };
-    auto scale = [&](int b) { return exp(-(double)b / PER_T); };
-    // `x` as a target among the whole numbers of bin b, which has some.
-    auto within = [&](int b, double x) {
-        const double y = (x - before(b)) / scale(b), most = (double)(s.sum[b] - 1);
-        return (uint64_t)(y > 0. ? (y < most ? y : most) : 0.);
+    const int listed = min((int)s.n, CAP);
+    auto pick = [&](auto counting, int b, uint64_t target) {
+        constexpr bool COUNT = decltype(counting)::value;
+        const uint32_t n = s.count[b] - counted(b);
+        return list ? select_in<T, true, COUNT>(s, z, p.V, g, listed, b, n, target) : select_in<T, false, COUNT>(s, z, p.V, g, 0, b, n, target);
     };
 
     double total = all;
     if (kb < BINS) {
-        const uint32_t rest = (uint32_t)p.top_k - counted(kb);  // of this bin, at least one
-        const Found f = select(std::true_type(), kb, rest - 1);
-        total = before(kb) + scale(kb) * (double)(f.sum + (uint64_t)(rest - f.count) * weight(logit_of(f.key)));
+        const Found f = pick(std::true_type(), kb, (uint64_t)p.top_k - counted(kb) - 1);
+        total = before(kb) + s.factor[kb] * (double)f.sum;
     }
     if (p.top_p < 1.f) {
         const double x = (double)p.top_p * total;
-        const int b = min(max(first_bin(s, cum >= x), pb0), pb1);
-        const double y = ceil((x - before(b)) / scale(b)) - 1.;  // a sum that reaches x passes the whole number below it
-        const uint64_t target = y > 0. ? (y < (double)(s.sum[b] - 1) ? (uint64_t)y : s.sum[b] - 1) : 0;
-        const Found f = select(std::false_type(), b, target);
-        const uint64_t w = max(weight(logit_of(f.key)), (uint64_t)1);
-        total = fmin(total, before(b) + scale(b) * (double)(f.sum + ((target - f.sum) / w + 1) * w));
+        const int b = min(max(reach(x, false), pb0), pb1);
+        const double y = ceil((x - before(b)) / s.factor[b]) - 1.;  // a sum that reaches x passes the whole number below it
+        const Found f = pick(std::false_type(), b, (uint64_t)fmax(y, 0.));
+        total = fmin(total, before(b) + s.factor[b] * (double)f.sum);
     }
-    if (mb < BINS) {
+    if (mb < BINS) {  // the last entry that is large enough
         uint64_t kept = 0;
-        entries(mb, [&](uint32_t key, uint32_t, uint64_t w) {
-            if (exp(((double)logit_of(key) - (double)z_max) * p.inv_t) >= (double)p.min_p) kept += w;
-        });
-        for (int o = 1; o < 64; o <<= 1) kept += (uint64_t)__shfl_xor((unsigned long long)kept, o);
+        const double least = p.log_min_p;
+        auto add = [&](float x, uint64_t w) {
+            if (((double)x - (double)z_max) * p.inv_t >= least) kept += w;
+        };
+        if (list) {
+            for (int i = tid; i < listed; i += PICK)
+                if ((int)(s.list[i].bin_weight >> 40) == mb) add(logit_of(s.list[i].rank), s.list[i].bin_weight & ((1ull << 40) - 1));
+        } else {
+            each_piece<T, PICK>(z, p.V, [&](int, const float(&v)[N]) {
+#pragma unroll 1
+                for (int j = 0; j < N; ++j) {
+                    double within;
+                    if (g.bin(v[j], within) == mb) add(v[j], g.weight(within));
+                }
+            });
+        }
         __syncthreads();
-        if (tid == 0) s.found_sum = 0;
+        if (tid == 0) s.sum_found = 0;
         __syncthreads();
-        if (tid % 64 == 0) atomicAdd((unsigned long long *)&s.found_sum, (unsigned long long)kept);
+        if (kept) atomicAdd(&s.sum_found, (unsigned long long)kept);
         __syncthreads();
-        total = fmin(total, before(mb) + scale(mb) * (double)s.found_sum);
-        __syncthreads();
+        total = fmin(total, before(mb) + s.factor[mb] * (double)s.sum_found);
     }
-    int b;
-    uint64_t target;
-    if (inside) {
-        b = min(max(target_bin(total), sb0), sb1);
-        target = within(b, (u > 0. ? u : 0.) * total);
-    } else {  // the last kept entry
-        b = min(max(last_bin(total), sb0), sb1);
-        const double y = rint((total - before(b)) / scale(b)) - 1.;
-        target = y > 0. ? (y < (double)(s.sum[b] - 1) ? (uint64_t)y : s.sum[b] - 1) : 0;
-    }
-    const Found f = select(std::false_type(), b, target);
-    const uint64_t w = max(weight(logit_of(f.key)), (uint64_t)1), nth = min((target - f.sum) / w, (uint64_t)f.ties - 1);
-    // Among equal ones by the index, smaller ones first.
-    const Found g = descend<true>(s, nth, [&](auto f2) {
-        entries(b, [&](uint32_t key, uint32_t index, uint64_t) {
-            if (key == f.key) f2(~index, 0);
-        });
-    });
+    const int b = min(max(token_bin(total), sb0), sb1);
+    const double x = ((inside ? fmax(u, 0.) * total : total) - before(b)) / s.factor[b];
+    const Found f = pick(std::false_type(), b, (uint64_t)fmax(inside ? x : rint(x) - 1., 0.));
     if (tid == 0) {
-        p.tok[row] = (int32_t)~g.key;
-        p.conf[row] = (float)((double)w * scale(b) / total);
+        p.tok[row] = (int32_t)~(uint32_t)f.rank;
+        p.conf[row] = (float)((double)f.weight * s.factor[b] / total);
     }
 }
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+template <typename T>
+void launch(const FcSampleArgs &p, hipStream_t s)
+{
+    const int parts = parts_of(p.V);
+    uint64_t *bins = (uint64_t *)p.workspace;
+    float *largest = (float *)((char *)p.workspace + align256((size_t)p.M * parts * BINS * sizeof(uint64_t)));
+    const dim3 grid((unsigned)(parts * p.M));
+    if (p.top_k > 0) k_sample_bins<T, true><<<grid, dim3(SCAN), 0, s>>>(p, parts, bins, largest);
+    else k_sample_bins<T, false><<<grid, dim3(SCAN), 0, s>>>(p, parts, bins, largest);
+    k_sample_pick<T><<<dim3((unsigned)p.M), dim3(PICK), 0, s>>>(p, parts, bins, largest);
+}
 
 }  // namespace
 
@@ -485,18 +553,14 @@ size_t fc_sample_workspace(int dtype, int M, int V)
     return align256(parts * BINS * sizeof(uint64_t)) + parts * sizeof(float);
 }
 
-hipError_t fc_launch_sample(const FcSampleArgs &p, int dtype, hipStream_t s)
+hipError_t fc_launch_sample(const FcSampleArgs &args, int dtype, hipStream_t s)
 {
-    const int parts = parts_of(p.V);
-    uint64_t *bins = (uint64_t *)p.workspace;
-    float *largest = (float *)((char *)p.workspace + align256((size_t)p.M * parts * BINS * sizeof(uint64_t)));
-    const dim3 grid((unsigned)parts, (unsigned)p.M);
-    if (dtype == FC_F32) {
-        k_sample_bins<float><<<grid, dim3(SCAN), 0, s>>>(p, parts, bins, largest);
-        k_sample_pick<float><<<dim3((unsigned)p.M), dim3(PICK), 0, s>>>(p, parts, bins, largest);
-    } else {
-        k_sample_bins<bf16_t><<<grid, dim3(SCAN), 0, s>>>(p, parts, bins, largest);
-        k_sample_pick<bf16_t><<<dim3((unsigned)p.M), dim3(PICK), 0, s>>>(p, parts, bins, largest);
-    }
+    FcSampleArgs p = args;
+    p.log_min_p = p.min_p > 0.f ? log((double)p.min_p) : 0.;
+    // With nothing but min-p to sum up to, entries below it need not be counted (two bins for the roundings).
+    p.last_bin = BINS - 1;
+    if (p.min_p > 0.f && !(p.top_p < 1.f) && -p.log_min_p * PER_T < BINS - 3) p.last_bin = (int)(-p.log_min_p * PER_T) + 2;
+    if (dtype == FC_F32) launch<float>(p, s);
+    else launch<bf16_t>(p, s);
     return hipGetLastError();
 }
