@@ -24,7 +24,8 @@ namespace {
 constexpr int BINS = 1024, PER_T = 32;       // bins; bins to a unit of z / T
 constexpr int SCAN = 512, PART = 16384;      // threads, and entries of a part: its counts fit 15 bits, its sums 47
 constexpr int PICK = 1024;                   // threads of the second kernel, one to a bin
-constexpr int CAP = 5120;                    // entries that it fetches into LDS
+constexpr int CAP = 12288;                   // entries that it fetches into LDS
+constexpr int LISTED = 256, LIST = 1024;     // entries that a part lists, about, and at most
 constexpr int FEW = 32;                      // entries that one wave compares with one another
 constexpr int SUM_BITS = 48;
 
@@ -77,29 +78,32 @@ struct Grid {
     }
 };
 
-// Entries of a row's piece of n, 16 bytes of a thread at a time: f(first index, values), -inf beyond the end.
+// 16 bytes of a row.
+template <typename T>
+struct Piece {
+    static constexpr int N = 16 / sizeof(T);
+    T v[N];
+    __device__ __forceinline__ void load(const T *z, int at, int n)  // -inf from n on
+    {
+        if (at + N <= n) *this = __builtin_bit_cast(Piece, fc_load_any<uint4>(z + at));
+        else
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[j] = at + j < n ? z[at + j] : fc_from_float<T>(-__builtin_inff());
+    }
+    __device__ __forceinline__ float get(int j) const { return fc_to_float(v[j]); }
+};
+
+// Every entry of a row's first n: f(index, logit).
 template <typename T, int THREADS, typename F>
-__device__ __forceinline__ void each_piece(const T *z, int n, F f)
+__device__ __forceinline__ void each_entry(const T *z, int n, F f)
 {
-    constexpr int N = 16 / sizeof(T);
-    struct Piece { T v[N]; };
+    constexpr int N = Piece<T>::N;
 #pragma unroll 1
-    for (int i0 = threadIdx.x * N; i0 < n; i0 += 2 * THREADS * N) {
-        Piece x[2];
+    for (int i0 = threadIdx.x * N; i0 < n; i0 += THREADS * N) {
+        Piece<T> x;
+        x.load(z, i0, n);
 #pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int at = i0 + k * THREADS * N;
-            if (at + N <= n) x[k] = __builtin_bit_cast(Piece, fc_load_any<uint4>(z + at));
-            else
-                for (int j = 0; j < N; ++j) x[k].v[j] = at + j < n ? z[at + j] : fc_from_float<T>(-__builtin_inff());
-        }
-#pragma unroll 1
-        for (int k = 0; k < 2; ++k) {
-            float v[N];
-#pragma unroll
-            for (int j = 0; j < N; ++j) v[j] = fc_to_float(k ? x[1].v[j] : x[0].v[j]);
-            f(i0 + k * THREADS * N, v);
-        }
+        for (int j = 0; j < N; ++j) f(i0 + j, x.get(j));
     }
 }
 
@@ -115,82 +119,110 @@ __device__ __forceinline__ X wave_scan(X x)
     return x;
 }
 
-// One part of a row: bins[] gets (entries << 48 | sum of weights).  With a top-k nothing below the part's own k-th entry can be kept, so its entries
-// are counted first and only those weighed: a count takes half the time of a weight and its sum (256 rows x 152064: see the figures at the launch).
-template <typename T, bool TOP_K>
-__global__ __launch_bounds__(SCAN) void k_sample_bins(FcSampleArgs p, int parts, uint64_t *__restrict__ bins, float *__restrict__ largest)
+// What is kept of a part besides its bins: the largest logit; the last bin of which the list has every entry (-1: none); their number.
+struct Part {
+    float largest;
+    int32_t bin;
+    uint32_t n;
+};
+
+// One part of a row: bins[] gets (entries << 48 | sum of weights), list[] the ranks of some 256 of its largest entries.
+//
+// The largest entries of the threads' pieces say where to end: at least as many entries as pieces reach a bin, so with a top-k nothing below the
+// bin that k pieces reach can be kept, and is not weighed; the list ends at the bin that 256 reach.
+template <typename T>
+__global__ __launch_bounds__(SCAN) void k_sample_bins(FcSampleArgs p, int parts, uint64_t *__restrict__ bins, uint64_t *__restrict__ list,
+                                                      Part *__restrict__ about)
 {
-    constexpr int N = 16 / sizeof(T);
+    constexpr int N = Piece<T>::N, PIECES = PART / (SCAN * N), U = PIECES / 4;  // (U pieces are eight values)
     __shared__ unsigned long long s_bin[BINS];
-    __shared__ uint32_t s_count[TOP_K ? BINS : 1], s_wave[SCAN / 64];
+    __shared__ uint32_t s_count[BINS], s_wave[SCAN / 64], s_n;
     __shared__ float s_max[SCAN / 64];
-    __shared__ int s_last;
+    __shared__ int s_last[2];
     const int tid = threadIdx.x;
     const uint32_t row = blockIdx.x / (uint32_t)parts, part = blockIdx.x - row * parts;
     const int from = part * PART, n = min(p.V - from, PART);
     const T *z = (const T *)p.logits + (size_t)row * p.ld + from;
-    float top = -__builtin_inff();
-    each_piece<T, SCAN>(z, n, [&](int, const float(&v)[N]) {
+    const size_t at = (size_t)row * parts + part;
+    Piece<T> x[PIECES];
+    float best[PIECES];
 #pragma unroll
-        for (int j = 0; j < N; ++j) top = fmaxf(top, v[j]);  // (NaN is passed over)
-    });
-    for (int i = tid; i < BINS; i += SCAN) {
-        s_bin[i] = 0;
-        if (TOP_K) s_count[i] = 0;
+    for (int i = 0; i < PIECES; ++i) x[i].load(z, (i * SCAN + tid) * N, n);
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i) {
+        best[i] = -__builtin_inff();
+#pragma unroll
+        for (int j = 0; j < N; ++j) best[i] = fmaxf(best[i], x[i].get(j));  // (NaN is passed over)
     }
+    float top = best[0];
+#pragma unroll
+    for (int i = 1; i < PIECES; ++i) top = fmaxf(top, best[i]);
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) top = fmaxf(top, __shfl_xor(top, o));
     if (tid % 64 == 0) s_max[tid / 64] = top;
-    if (tid == 0) s_last = BINS - 1;
+    for (int i = tid; i < BINS; i += SCAN) {
+        s_bin[i] = 0;
+        s_count[i] = 0;
+    }
+    if (tid == 0) {
+        s_last[0] = s_last[1] = BINS;
+        s_n = 0;
+    }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < SCAN / 64; ++i) top = fmaxf(top, s_max[i]);
+    int end = -1;
     if (top > -__builtin_inff()) {
         const Grid g(top, p.inv_t * PER_T);
-        int last = min(p.last_bin, BINS - 1);
-        if constexpr (TOP_K) {
-            const float cut = g.lowest(last);
-            each_piece<T, SCAN>(z, n, [&](int, const float(&v)[N]) {
+        // (in fp32: at most two bins above the exact one)
+        const float c = (float)g.c;
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const float d = g.infinite ? (best[i] == top ? 0.f : (float)BINS) : (top - best[i]) * c;
+            if (d < (float)BINS) atomicAdd(&s_count[(int)d], 1u);
+        }
+        __syncthreads();
+        const uint32_t a = s_count[2 * tid], b = s_count[2 * tid + 1];
+        uint32_t run = wave_scan(a + b);
+        if (tid % 64 == 63) s_wave[tid / 64] = run;
+        __syncthreads();
+        for (int i = 0; i < tid / 64; ++i) run += s_wave[i];
+        const uint32_t ks[2] = {p.top_k > 0 ? (uint32_t)p.top_k : 0xffffffffu, (uint32_t)min(max(p.top_k, LISTED), 2 * LISTED)};
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (run >= ks[i] && run - a - b < ks[i]) s_last[i] = run - b >= ks[i] ? 2 * tid : 2 * tid + 1;
+        __syncthreads();
+        const int last = min(min(p.last_bin, BINS - 1), s_last[0] + 2);
+        end = min(last, s_last[1] + 2);
+        const float cut = g.lowest(last);
+        // Eight values a turn, then the pieces move up: short code, and registers that no index picks.
+#pragma unroll 1
+        for (int i = 0; i < PIECES; i += U) {
+#pragma unroll
+            for (int k = 0; k < U; ++k)
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
+                    const float v = x[k].get(j);
+                    if (!(v >= cut)) continue;
                     double within;
-                    if (v[j] >= cut) {
-                        const int b = g.bin(v[j], within);
-                        if (b < BINS) atomicAdd(&s_count[b], 1u);
-                    }
+                    const int bin = g.bin(v, within);
+                    if (bin > last) continue;
+                    atomicAdd(&s_bin[bin], (unsigned long long)(1ull << SUM_BITS | g.weight(within)));
+                    if (bin > end) continue;
+                    const uint32_t to = atomicAdd(&s_n, 1u);
+                    if (to < LIST) list[at * LIST + to] = rank_of(v, (uint32_t)(from + ((i + k) * SCAN + tid) * N + j));
                 }
-            });
-            __syncthreads();
-            const uint32_t a = s_count[2 * tid], b = s_count[2 * tid + 1];
-            uint32_t run = wave_scan(a + b);
-            if (tid % 64 == 63) s_wave[tid / 64] = run;
-            __syncthreads();
-            for (int i = 0; i < tid / 64; ++i) run += s_wave[i];
-            const uint32_t k = (uint32_t)p.top_k, first = run - b;
-            if (run >= k && run - a - b < k) s_last = first >= k ? 2 * tid : 2 * tid + 1;
-            __syncthreads();
-            last = min(last, s_last);
-        }
-        const float cut = g.lowest(last);
-        each_piece<T, SCAN>(z, n, [&](int, const float(&v)[N]) {
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                double within;
-                if (v[j] >= cut) {
-                    const int b = g.bin(v[j], within);
-                    if (b <= last) atomicAdd(&s_bin[b], (unsigned long long)(1ull << SUM_BITS | g.weight(within)));
-                }
-            }
-        });
+            for (int k = 0; k + U < PIECES; ++k) x[k] = x[k + U];
+        }
     }
     __syncthreads();
-    const size_t at = (size_t)row * parts + part;
     for (int i = tid; i < BINS; i += SCAN) bins[at * BINS + i] = s_bin[i];
-    if (tid == 0) largest[at] = top;
+    if (tid == 0) about[at] = Part{top, s_n <= LIST ? end : -1, min(s_n, (uint32_t)LIST)};
 }
 
 struct Entry {
-    uint64_t rank, bin_weight;  // bin << 40 | weight
+    uint64_t rank, weight;
 };
 
 struct PickShared {
@@ -198,8 +230,7 @@ struct PickShared {
     double factor[BINS];    // exp(-bin / 32)
     uint32_t count[BINS];   // running counts
     uint64_t sum[BINS];     // the bins' own sums
-    Entry list[CAP];
-    uint8_t marked[BINS];
+    uint64_t list[CAP];     // ranks
     double wave_sum[PICK / 64];
     uint32_t wave_count[PICK / 64];
     uint64_t digit_sum[256];
@@ -239,7 +270,12 @@ __device__ Found select(PickShared &s, uint32_t n, uint64_t target, EACH each)
             a = min(a, rank);
             b = max(b, rank);
         });
-        if (a <= b) {
+#pragma unroll 1
+        for (int o = 1; o < 64; o <<= 1) {
+            a = min(a, (uint64_t)__shfl_xor((unsigned long long)a, o));
+            b = max(b, (uint64_t)__shfl_xor((unsigned long long)b, o));
+        }
+        if (a <= b && tid % 64 == 0) {
             atomicMin(&s.low, (unsigned long long)a);
             atomicMax(&s.high, (unsigned long long)b);
         }
@@ -307,59 +343,55 @@ __device__ Found select(PickShared &s, uint32_t n, uint64_t target, EACH each)
         uint32_t runs = 0;
         for (uint32_t i = 0; i < n; ++i)
             if (s.few[i].rank > own.rank) {
-                run += s.few[i].bin_weight;
+                run += s.few[i].weight;
                 ++runs;
             }
-        const bool passes = COUNT ? count + runs + 1 > target : run + own.bin_weight > target;
+        const bool passes = COUNT ? count + runs + 1 > target : run + own.weight > target;
         const bool before = COUNT ? count + runs > target : run > target;
         if ((passes && !before) || (!passes && runs == n - 1)) {
             s.rank_found = own.rank;
-            s.sum_found = run + own.bin_weight;
-            s.weight_found = own.bin_weight;
+            s.sum_found = run + own.weight;
+            s.weight_found = own.weight;
         }
     }
     __syncthreads();
     return Found{s.rank_found, s.sum_found, s.weight_found};
 }
 
-// The entries of bin b: those of the list, or (LIST false) found in the row once more.
+// The entries of bin b, n of them, in the list or (LIST false) in the row.
 template <typename T, bool LIST, bool COUNT>
 __device__ __attribute__((noinline)) Found select_in(PickShared &s, const T *z, int V, const Grid &g, int listed, int b, uint32_t n, uint64_t target)
 {
-    if constexpr (LIST) {
-        return select<COUNT>(s, n, target, [&](auto f) {
-            for (int i = threadIdx.x; i < listed; i += PICK) {
-                const Entry e = s.list[i];
-                if ((int)(e.bin_weight >> 40) == b) f(e.rank, e.bin_weight & ((1ull << 40) - 1));
-            }
-        });
-    } else {
-        const float low = g.lowest(b), high = g.highest(b);
-        constexpr int N = 16 / sizeof(T);
-        return select<COUNT>(s, n, target, [&](auto f) {
-            each_piece<T, PICK>(z, V, [&](int at, const float(&v)[N]) {
+    const float low = g.lowest(b), high = g.highest(b);
+    return select<COUNT>(s, n, target, [&](auto f) {
+        double within;
+        if constexpr (LIST) {
 #pragma unroll 1
-                for (int j = 0; j < N; ++j) {
-                    double within;
-                    if (v[j] >= low && v[j] <= high && g.bin(v[j], within) == b) f(rank_of(v[j], (uint32_t)(at + j)), g.weight(within));
-                }
+            for (int i = threadIdx.x; i < listed; i += PICK) {
+                const uint64_t rank = s.list[i];
+                const float x = logit_of(rank);
+                if (x >= low && x <= high && g.bin(x, within) == b) f(rank, g.weight(within));
+            }
+        } else {
+            each_entry<T, PICK>(z, V, [&](int i, float x) {
+                if (x >= low && x <= high && g.bin(x, within) == b) f(rank_of(x, (uint32_t)i), g.weight(within));
             });
-        });
-    }
+        }
+    });
 }
 
 template <typename T>
-__global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts, const uint64_t *__restrict__ bins, const float *__restrict__ largest)
+__global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts, const uint64_t *__restrict__ bins, const uint64_t *__restrict__ lists,
+                                                      const Part *__restrict__ abouts)
 {
     __shared__ PickShared s;
-    constexpr int N = 16 / sizeof(T);
     const int tid = threadIdx.x, row = blockIdx.x;
     const T *z = (const T *)p.logits + (size_t)row * p.ld;
-    const float *most = largest + (size_t)row * parts;
-    const uint64_t *part = bins + (size_t)row * parts * BINS;
+    const Part *about = abouts + (size_t)row * parts;
+    const uint64_t *part = bins + (size_t)row * parts * BINS, *lst = lists + (size_t)row * parts * LIST;
 
     float z_max = -__builtin_inff();
-    for (int i = tid % 64; i < parts; i += 64) z_max = fmaxf(z_max, most[i]);
+    for (int i = tid % 64; i < parts; i += 64) z_max = fmaxf(z_max, about[i].largest);
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) z_max = fmaxf(z_max, __shfl_xor(z_max, o));
     if (z_max == -__builtin_inff()) {
@@ -371,17 +403,38 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
     }
     const Grid g(z_max, p.inv_t * PER_T);
 
-    // Thread i: bin i of the row.
+    // Thread i: bin i of the row, eight parts in flight together.  (lists_to: the last bin of which the parts' lists have every entry.)
     uint32_t count = 0;
     uint64_t sum = 0;
-#pragma unroll 4
-    for (int i = 0; i < parts; ++i) {
+    int lists_to = BINS;
+#pragma unroll 1
+    for (int i0 = 0; i0 < parts; i0 += 64) {
+        // (lane: part; one of nothing is in no bin)
         double within;
-        const int at = tid - g.bin(most[i], within);  // (a part of nothing is in no bin)
-        const uint64_t x = part[(size_t)i * BINS + max(at, 0)];
-        count += at >= 0 ? (uint32_t)(x >> SUM_BITS) : 0;
-        sum += at >= 0 ? x & ((1ull << SUM_BITS) - 1) : 0;
+        const int mine = i0 + tid % 64;
+        const Part a = about[min(mine, parts - 1)];
+        const int off = mine < parts ? g.bin(a.largest, within) : BINS;
+        lists_to = min(lists_to, off < BINS ? (a.bin < 0 ? -1 : off + a.bin) : BINS);
+        const int m = min(parts - i0, 64);
+#pragma unroll 1
+        for (int i = 0; i < m; i += 8) {
+            uint64_t x[8];
+            int at[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int from = min(i + k, m - 1);
+                at[k] = i + k < m ? tid - __builtin_amdgcn_readlane(off, from) : -1;
+                x[k] = part[(size_t)(i0 + from) * BINS + max(at[k], 0)];
+            }
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                count += at[k] >= 0 ? (uint32_t)(x[k] >> SUM_BITS) : 0;
+                sum += at[k] >= 0 ? x[k] & ((1ull << SUM_BITS) - 1) : 0;
+            }
+        }
     }
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) lists_to = min(lists_to, __shfl_xor(lists_to, o));
     const double factor = exp(-(double)tid / PER_T);
     double cum = wave_scan((double)sum * factor);
     uint32_t counts = wave_scan(count);
@@ -391,7 +444,6 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
     }
     s.sum[tid] = sum;
     s.factor[tid] = factor;
-    s.marked[tid] = 0;
     if (tid == 0) s.n = 0;
     __syncthreads();
     for (int i = 0; i < tid / 64; ++i) {
@@ -446,38 +498,57 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
         }
     }
     const int sb0 = token_bin(low), sb1 = low < high ? token_bin(high) : sb0;
-    const bool filter = tid == kb || tid == mb || (tid >= pb0 && tid <= pb1), mark = filter || (tid >= sb0 && tid <= sb1);
-    s.marked[tid] = mark;
-    if (mark && count) atomicAdd(&s.n, count);
-    // Logits of the filters' bins, and of the token's.
-    const int f0 = min(min(kb, mb), pb0), f1 = max(max(kb < BINS ? kb : -1, mb < BINS ? mb : -1), pb1);
-    const float flow = f1 < 0 ? __builtin_inff() : g.lowest(f1), fhigh = f1 < 0 ? -__builtin_inff() : g.highest(f0);
-    const float slow = g.lowest(sb1), shigh = g.highest(sb0);
+    // Logits of the bin in which top-k ends, of those in which the other filters can, and of the token's.  Where they lie apart with many entries between
+    // them, three ranges; else one.
+    const int f0 = min(pb0, mb), f1 = max(mb < BINS ? mb : -1, pb1), first = min(min(f0, kb), sb0), final = max(max(f1, kb < BINS ? kb : -1), sb1);
+    const bool apart = s.count[final] - counted(first) > CAP / 2;
+    const float none = __builtin_inff();
+    const float slow = g.lowest(apart ? sb1 : final), shigh = g.highest(apart ? sb0 : first);
+    const float flow = apart && f1 >= 0 ? g.lowest(f1) : none, fhigh = apart && f1 >= 0 ? g.highest(f0) : -none;
+    const float klow = apart && kb < BINS ? g.lowest(kb) : none, khigh = apart && kb < BINS ? g.highest(kb) : -none;
+    auto wanted = [&](float x) { return (x >= slow && x <= shigh) || (apart && ((x >= flow && x <= fhigh) || (x >= klow && x <= khigh))); };
+    auto take = [&](uint64_t rank) {
+        const uint32_t to = atomicAdd(&s.n, 1u);
+        if (to < CAP) s.list[to] = rank;
+    };
+    if (final <= lists_to) {  // a wave to a part
+#pragma unroll 1
+        for (int i = tid / 64; i < parts; i += PICK / 64) {
+            const uint32_t n = about[i].n;
+#pragma unroll 1
+            for (uint32_t j0 = tid % 64; j0 < n; j0 += 4 * 64) {
+                uint64_t r[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) r[k] = lst[(size_t)i * LIST + min(j0 + k * 64, n - 1)];
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (j0 + k * 64 < n && wanted(logit_of(r[k]))) take(r[k]);
+            }
+        }
+    } else {  // eight pieces of a thread in flight together
+        constexpr int N = Piece<T>::N, U = 8;
+#pragma unroll 1
+        for (int i0 = tid * N; i0 < p.V; i0 += U * PICK * N) {
+            Piece<T> x[U];
+#pragma unroll
+            for (int k = 0; k < U; ++k) x[k].load(z, i0 + k * PICK * N, p.V);
+            if (apart) {
+#pragma unroll
+                for (int k = 0; k < U; ++k)
+#pragma unroll
+                    for (int j = 0; j < N; ++j)
+                        if (wanted(x[k].get(j))) take(rank_of(x[k].get(j), (uint32_t)(i0 + k * PICK * N + j)));
+            } else {
+#pragma unroll
+                for (int k = 0; k < U; ++k)
+#pragma unroll
+                    for (int j = 0; j < N; ++j)
+                        if (x[k].get(j) >= slow && x[k].get(j) <= shigh) take(rank_of(x[k].get(j), (uint32_t)(i0 + k * PICK * N + j)));
+            }
+        }
+    }
     __syncthreads();
     const bool list = s.n <= (uint32_t)CAP;
-    __syncthreads();
-    if (tid == 0) s.n = 0;
-    __syncthreads();
-    if (list) {
-        each_piece<T, PICK>(z, p.V, [&](int at, const float(&v)[N]) {
-            uint32_t hit = 0;
-#pragma unroll
-            for (int j = 0; j < N; ++j) hit |= ((v[j] >= slow && v[j] <= shigh) || (v[j] >= flow && v[j] <= fhigh) ? 1u : 0u) << j;
-            while (hit) {
-                const int j = __builtin_ctz(hit);
-                hit &= hit - 1;
-                float x = v[0];
-#pragma unroll
-                for (int i = 1; i < N; ++i) x = j == i ? v[i] : x;
-                double within;
-                const int b = g.bin(x, within);
-                if (b >= BINS || !s.marked[b]) continue;
-                const uint32_t to = atomicAdd(&s.n, 1u);
-                if (to < CAP) s.list[to] = Entry{rank_of(x, (uint32_t)(at + j)), (uint64_t)b << 40 | g.weight(within)};
-            }
-        });
-        __syncthreads();
-    }
     const int listed = min((int)s.n, CAP);
     auto pick = [&](auto counting, int b, uint64_t target) {
         constexpr bool COUNT = decltype(counting)::value;
@@ -499,21 +570,16 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
     }
     if (mb < BINS) {  // the last entry that is large enough
         uint64_t kept = 0;
-        const double least = p.log_min_p;
-        auto add = [&](float x, uint64_t w) {
-            if (((double)x - (double)z_max) * p.inv_t >= least) kept += w;
+        const float mlow = g.lowest(mb), mhigh = g.highest(mb);
+        auto look = [&](float x) {
+            double within;
+            if (x >= mlow && x <= mhigh && g.bin(x, within) == mb && ((double)x - (double)z_max) * p.inv_t >= p.log_min_p) kept += g.weight(within);
         };
         if (list) {
-            for (int i = tid; i < listed; i += PICK)
-                if ((int)(s.list[i].bin_weight >> 40) == mb) add(logit_of(s.list[i].rank), s.list[i].bin_weight & ((1ull << 40) - 1));
-        } else {
-            each_piece<T, PICK>(z, p.V, [&](int, const float(&v)[N]) {
 #pragma unroll 1
-                for (int j = 0; j < N; ++j) {
-                    double within;
-                    if (g.bin(v[j], within) == mb) add(v[j], g.weight(within));
-                }
-            });
+            for (int i = tid; i < listed; i += PICK) look(logit_of(s.list[i]));
+        } else {
+            each_entry<T, PICK>(z, p.V, [&](int, float x) { look(x); });
         }
         __syncthreads();
         if (tid == 0) s.sum_found = 0;
@@ -533,25 +599,33 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
+// Workspace: the parts' bins, their lists, and what is said about them.
+struct Space {
+    size_t lists, abouts, total;
+    Space(int M, int V)
+    {
+        const size_t parts = (size_t)M * parts_of(V);
+        lists = align256(parts * BINS * sizeof(uint64_t));
+        abouts = lists + align256(parts * LIST * sizeof(uint64_t));
+        total = abouts + parts * sizeof(Part);
+    }
+};
+
 template <typename T>
 void launch(const FcSampleArgs &p, hipStream_t s)
 {
     const int parts = parts_of(p.V);
-    uint64_t *bins = (uint64_t *)p.workspace;
-    float *largest = (float *)((char *)p.workspace + align256((size_t)p.M * parts * BINS * sizeof(uint64_t)));
-    const dim3 grid((unsigned)(parts * p.M));
-    if (p.top_k > 0) k_sample_bins<T, true><<<grid, dim3(SCAN), 0, s>>>(p, parts, bins, largest);
-    else k_sample_bins<T, false><<<grid, dim3(SCAN), 0, s>>>(p, parts, bins, largest);
-    k_sample_pick<T><<<dim3((unsigned)p.M), dim3(PICK), 0, s>>>(p, parts, bins, largest);
+    const Space w(p.M, p.V);
+    char *at = (char *)p.workspace;
+    uint64_t *bins = (uint64_t *)at, *lists = (uint64_t *)(at + w.lists);
+    Part *abouts = (Part *)(at + w.abouts);
+    k_sample_bins<T><<<dim3((unsigned)(parts * p.M)), dim3(SCAN), 0, s>>>(p, parts, bins, lists, abouts);
+    k_sample_pick<T><<<dim3((unsigned)p.M), dim3(PICK), 0, s>>>(p, parts, bins, lists, abouts);
 }
 
 }  // namespace
 
-size_t fc_sample_workspace(int dtype, int M, int V)
-{
-    const size_t parts = (size_t)M * parts_of(V);
-    return align256(parts * BINS * sizeof(uint64_t)) + parts * sizeof(float);
-}
+size_t fc_sample_workspace(int dtype, int M, int V) { return Space(M, V).total; }
 
 hipError_t fc_launch_sample(const FcSampleArgs &args, int dtype, hipStream_t s)
 {
