@@ -26,7 +26,7 @@ constexpr int SCAN = 512, PART = 16384;      // threads, and entries of a part: 
 constexpr int PICK = 1024;                   // threads of the second kernel, one to a bin
 constexpr int CAP = 12288;                   // entries that it fetches into LDS
 constexpr int LISTED = 256, LIST = 1024;     // entries that a part lists, about, and at most
-constexpr int FEW = 32;                      // entries that one wave compares with one another
+constexpr int FEW = 64;                      // entries that one wave compares with one another
 constexpr int SUM_BITS = 48;
 
 __host__ __device__ inline int parts_of(int V) { return (V + PART - 1) / PART; }
@@ -139,6 +139,7 @@ __global__ __launch_bounds__(SCAN) void k_sample_bins(FcSampleArgs p, int parts,
     __shared__ uint32_t s_count[BINS], s_wave[SCAN / 64], s_n;
     __shared__ float s_max[SCAN / 64];
     __shared__ int s_last[2];
+    __shared__ uint64_t s_queue[SCAN / 64][64 + 8 * 64];
     const int tid = threadIdx.x;
     const uint32_t row = blockIdx.x / (uint32_t)parts, part = blockIdx.x - row * parts;
     const int from = part * PART, n = min(p.V - from, PART);
@@ -195,25 +196,59 @@ __global__ __launch_bounds__(SCAN) void k_sample_bins(FcSampleArgs p, int parts,
         const int last = min(min(p.last_bin, BINS - 1), s_last[0] + 2);
         end = min(last, s_last[1] + 2);
         const float cut = g.lowest(last);
-        // Eight values a turn, then the pieces move up: short code, and registers that no index picks.
+        // Eight values a turn, then the pieces move up: short code, and registers that no index picks.  Where most lanes have nothing that matters,
+        // entries pass through a queue of the wave's, so that all its lanes weigh: under a top-k of 50 one entry in hundreds does (32 x 152064
+        // bf16: 30 us with the queue, 48 without), with none at temperature 1 all do (33 x 32001 fp32: 18 us with it, 13.5 without).
+        uint64_t *queue = s_queue[tid / 64];
+        uint32_t held = 0;
+        auto weigh = [&](float v, int i) {
+            double within;
+            const int bin = g.bin(v, within);
+            if (bin > last) return;
+            atomicAdd(&s_bin[bin], (unsigned long long)(1ull << SUM_BITS | g.weight(within)));
+            if (bin > end) return;
+            const uint32_t to = atomicAdd(&s_n, 1u);
+            if (to < LIST) list[at * LIST + to] = rank_of(v, (uint32_t)(from + i));
+        };
 #pragma unroll 1
         for (int i = 0; i < PIECES; i += U) {
+            int in = 0;
 #pragma unroll
             for (int k = 0; k < U; ++k)
 #pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    const float v = x[k].get(j);
-                    if (!(v >= cut)) continue;
-                    double within;
-                    const int bin = g.bin(v, within);
-                    if (bin > last) continue;
-                    atomicAdd(&s_bin[bin], (unsigned long long)(1ull << SUM_BITS | g.weight(within)));
-                    if (bin > end) continue;
-                    const uint32_t to = atomicAdd(&s_n, 1u);
-                    if (to < LIST) list[at * LIST + to] = rank_of(v, (uint32_t)(from + ((i + k) * SCAN + tid) * N + j));
-                }
+                for (int j = 0; j < N; ++j) in += __builtin_popcountll(__ballot(x[k].get(j) >= cut));
+            if (in >= 64 * U * N / 2) {
+#pragma unroll
+                for (int k = 0; k < U; ++k)
+#pragma unroll
+                    for (int j = 0; j < N; ++j)
+                        if (x[k].get(j) >= cut) weigh(x[k].get(j), ((i + k) * SCAN + tid) * N + j);
+            } else if (in) {
+#pragma unroll
+                for (int k = 0; k < U; ++k)
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        const float v = x[k].get(j);
+                        const uint64_t mask = __ballot(v >= cut);
+                        const uint32_t to = __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, held));
+                        if (v >= cut) queue[to] = (uint64_t)__float_as_uint(v) << 32 | (uint32_t)(((i + k) * SCAN + tid) * N + j);
+                        held += (uint32_t)__builtin_popcountll(mask);
+                    }
+            }
 #pragma unroll
             for (int k = 0; k + U < PIECES; ++k) x[k] = x[k + U];
+            const bool more = i + U < PIECES;
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll 1
+            while (held >= 64 || (!more && held)) {
+                const uint32_t n = min(held, 64u);
+                held -= n;
+                if ((uint32_t)(tid % 64) < n) {
+                    const uint64_t e = queue[held + tid % 64];
+                    weigh(__uint_as_float((uint32_t)(e >> 32)), (int)(uint32_t)e);
+                }
+            }
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
     }
     __syncthreads();
@@ -356,6 +391,45 @@ __device__ Found select(PickShared &s, uint32_t n, uint64_t target, EACH each)
     }
     __syncthreads();
     return Found{s.rank_found, s.sum_found, s.weight_found};
+}
+
+// What select() finds, in one wave without a barrier: entries of bin b in the list, FEW at most.
+template <bool COUNT>
+__device__ __attribute__((noinline)) Found select_few(PickShared &s, const Grid &g, int listed, int b, uint64_t target)
+{
+    const int lane = threadIdx.x;
+    const float low = g.lowest(b), high = g.highest(b);
+    uint32_t n = 0;
+#pragma unroll 1
+    for (int i = lane; i - lane < listed; i += 64) {
+        const uint64_t rank = s.list[min(i, listed - 1)];
+        const float x = logit_of(rank);
+        double within;
+        const bool in = i < listed && x >= low && x <= high && g.bin(x, within) == b;
+        const uint64_t mask = __ballot(in);
+        const uint32_t to = __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, n));
+        if (in && to < FEW) s.few[to] = Entry{rank, g.weight(within)};
+        n += (uint32_t)__builtin_popcountll(mask);
+    }
+    n = min(n, (uint32_t)FEW);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const Entry own = s.few[lane];
+    uint64_t run = 0;
+    uint32_t runs = 0;
+#pragma unroll 1
+    for (uint32_t i = 0; i < n; ++i) {
+        const Entry e = s.few[i];
+        if (e.rank > own.rank) {
+            run += e.weight;
+            ++runs;
+        }
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    const uint64_t to = run + own.weight;
+    const bool passes = COUNT ? runs + 1 > target : to > target, before = COUNT ? runs > target : run > target;
+    const uint64_t mask = __ballot((uint32_t)lane < n && ((passes && !before) || (!passes && runs == n - 1)));
+    const int at = mask ? __builtin_ctzll(mask) : 0;
+    return Found{(uint64_t)__shfl((unsigned long long)own.rank, at), (uint64_t)__shfl((unsigned long long)to, at), (uint64_t)__shfl((unsigned long long)own.weight, at)};
 }
 
 // The entries of bin b, n of them, in the list or (LIST false) in the row.
@@ -550,8 +624,17 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
     __syncthreads();
     const bool list = s.n <= (uint32_t)CAP;
     const int listed = min((int)s.n, CAP);
+    // Where no bin in question has more entries than a wave has lanes, its first wave goes on alone.
+    const bool asked = tid == kb || tid == mb || (tid >= pb0 && tid <= pb1) || (tid >= sb0 && tid <= sb1);
+    const bool alone = list && listed <= 4096 && !__syncthreads_or(asked && count > FEW);
+    if (alone && tid >= 64) return;
+    auto sync = [&] {
+        if (alone) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        else __syncthreads();
+    };
     auto pick = [&](auto counting, int b, uint64_t target) {
         constexpr bool COUNT = decltype(counting)::value;
+        if (alone) return select_few<COUNT>(s, g, listed, b, target);
         const uint32_t n = s.count[b] - counted(b);
         return list ? select_in<T, true, COUNT>(s, z, p.V, g, listed, b, n, target) : select_in<T, false, COUNT>(s, z, p.V, g, 0, b, n, target);
     };
@@ -577,15 +660,15 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
         };
         if (list) {
 #pragma unroll 1
-            for (int i = tid; i < listed; i += PICK) look(logit_of(s.list[i]));
+            for (int i = tid; i < listed; i += alone ? 64 : PICK) look(logit_of(s.list[i]));
         } else {
             each_entry<T, PICK>(z, p.V, [&](int, float x) { look(x); });
         }
-        __syncthreads();
+        sync();
         if (tid == 0) s.sum_found = 0;
-        __syncthreads();
+        sync();
         if (kept) atomicAdd(&s.sum_found, (unsigned long long)kept);
-        __syncthreads();
+        sync();
         total = fmin(total, before(mb) + s.factor[mb] * (double)s.sum_found);
     }
     const int b = min(max(token_bin(total), sb0), sb1);
