@@ -1,4 +1,4 @@
-// Bidirectional attention over a cache held in 4 bits (bf16 queries).
+// Bidirectional attention over a cache held in 4 bits.
 //
 // S^T = K Q^T, softmax weights in registers, O^T = V^T W^T, one pass over the keys.  A wave holds 16 RT query rows (the rows of all
 // query heads that share a kv head are one list) and takes tiles of 64 keys, straight from memory into operand registers: the
@@ -6,13 +6,17 @@
 //
 //  - Scores.  The 16x16x128 matrix instruction with block scales takes the key codes and their scales as they are stored; with a 6-bit other operand
 //    it takes 16 clocks, a quarter of what bfloat16 products of that size take.  What a query lacks in bits it gets by parts: a lane's 32
-//    elements of a row are three E2M3 numbers each, every one the rounding error of those before, 2^-16 of the largest of the 32 in the
+//    elements of a row are three E2M3 numbers each, every one the rounding error of those before, 2^-14 of the largest of the 32 in the
 //    end (the rows are bfloat16).  48 clocks, and no key is ever converted.  (Two e4m3 parts: 64 clocks.)
 //  - Weights.  Value row t is codes times 2^e_t.  The power goes into the exponent of the row's weight, w_t = 2^(s_t + e_t - r), so the codes
 //    are multiplied as they are, and the sum that divides adds w_t 2^-e_t.  The key multiply starts from e_t over the softmax scale, so this
 //    costs nothing.  The reference r only has to keep w_t in range: it moves when a score passes it by 2^MOVE, which after the first
 //    tiles is rare.  Weights are rounded to fp16 (11 bits; bfloat16 would add as much error as rounding the output does, two E2M3 parts
 //    more, 2.8e-3 for 1.7e-3 relative in all), sums are fp32.
+//  - fp32 rows have six parts (2^-29 of the largest), and a weight is two fp16 numbers, the second in units of 2^-12 with sums of its own: 2^-23 of
+//    the weight.  The reference is a whole number and e_t - r is added with the scale, so a score is rounded once.  Errors against 64 bits are
+//    1e-7 .. 2e-7, a quarter of a plain fp32 computation's; 1 x 32 rows x 28 heads over 1056 keys take 9.1 us (bfloat16: 6.7; one wave per row
+//    with plain fp32 arithmetic took 46 us for 8 rows x 4 heads over 96 keys, where this takes 4.6).
 //  - Values.  Codes become fp16 pairs by one conversion each, once for all RT row tiles.
 //
 // The waves of a workgroup take tiles in turn and add up in LDS at the end.  Where there are few (sequence, kv head, row group)
@@ -37,12 +41,14 @@ typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u6 __attribute__((ext_vector_type(6)));
 
 constexpr float MOVE = 8.f;  // a score may pass the reference by 2^MOVE
+constexpr float FINE = 4096.f;  // fp32: what a weight's fp16 lacks is multiplied in units of 1 / FINE
+template <typename T> constexpr int MOST_RT = sizeof(T) == 4 ? 1 : 2;  // row tiles of a workgroup
 
 struct AttnArgs {
-    const bf16_t *q;
+    const void *q;
     const uint8_t *layer;
     const int32_t *pos, *lens;
-    bf16_t *out;
+    void *out;
     float *part;  // partial results: [pair][split][rows][DH], then [pair][split][rows][2] (reference, sum)
     int A, kv_len, Hq, Hkv, g, tiles, rows, groups, splits, units;
     float c, by_c;  // scale * log2(e), and 1 / that
@@ -97,52 +103,82 @@ __device__ __forceinline__ f4 multiply(const i8x &codes, uint32_t sa, const i8x 
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(codes, part, acc, 4, 2, SA, (int)sa, SB, (int)sb);
 }
 
-// Query rows as operands: N multiplies of a row tile, with the scales in one word.  Heads of 128: three parts, a multiply each.  Heads of 64: the
-// first two parts are the two halves of one multiply (the lower lanes' keys against the first, the upper lanes' against the second), the
-// third one half of another.
-template <int DH, int RT>
+// 32 elements of a query row, even and odd ones, and the largest one's bits.
+__device__ __forceinline__ uint32_t query_row(const bf16_t *q, f16x &a, f16x &b)
+{
+    u4 raw[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) raw[i] = fc_load_any<u4>(q + i * 8);
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        a[i] = __uint_as_float(raw[i / 4][i % 4] << 16);
+        b[i] = __uint_as_float(raw[i / 4][i % 4] & 0xffff0000u);
+        top = max(top, max(__float_as_uint(a[i]) & 0x7fffffffu, __float_as_uint(b[i]) & 0x7fffffffu));
+    }
+    return top;
+}
+__device__ __forceinline__ uint32_t query_row(const float *q, f16x &a, f16x &b)
+{
+    f4 raw[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) raw[i] = fc_load_any<f4>(q + i * 4);
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        a[i] = raw[i / 2][i % 2 * 2];
+        b[i] = raw[i / 2][i % 2 * 2 + 1];
+        top = max(top, max(__float_as_uint(a[i]) & 0x7fffffffu, __float_as_uint(b[i]) & 0x7fffffffu));
+    }
+    return top;
+}
+
+// Query rows as operands: N multiplies of a row tile, PARTS of 6 bits.  Heads of 128: a multiply each.  Heads of 64: a part is half a multiply (the
+// lower lanes' keys against an even one, the upper lanes' against the next; the sixth half of three parts is zero).
+template <typename T, int DH, int RT>
 struct Queries {
-    static constexpr int N = DH == 128 ? 3 : 2;
+    static constexpr int PARTS = sizeof(T) == 4 ? 6 : 3, N = DH == 128 ? PARTS : (PARTS + 1) / 2;
     u4 lo[RT][N][64];
     u2 hi[RT][N][64];
-    uint32_t scale[RT][64];
+    uint32_t scale[RT][(N + 3) / 4][64];
 
-    __device__ __forceinline__ void fill(const bf16_t *q, int rt, int lane)  // q: the lane's 32 elements
+    __device__ __forceinline__ void fill(const T *q, int rt, int lane)  // q: the lane's 32 elements
     {
-        u4 raw[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) raw[i] = fc_load_any<u4>(q + i * 8);
         f16x a, b;
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            a[i] = __uint_as_float(raw[i / 4][i % 4] << 16);
-            b[i] = __uint_as_float(raw[i / 4][i % 4] & 0xffff0000u);
-            top = max(top, max(__float_as_uint(a[i]) & 0x7fffffffu, __float_as_uint(b[i]) & 0x7fffffffu));
-        }
-        // the largest goes to 4 .. 7.5; below 2^-88 nothing need be exact
+        const uint32_t top = query_row(q, a, b);
+        // The largest goes to 4 .. 7.5; below 2^-88 nothing need be exact.  At most a quarter of a unit is left: 4 in units of 2^-4, and of
+        // that an eighth: 4 in units of 2^-5.
         const uint32_t e = max((top >> 23) + ((top & 0x7fffffu) > 0x700000u ? 1 : 0), 40u) - 2;
-        u6 part[3];
-        part[0] = to_6bit(a, b, __uint_as_float(e << 23));
-        less_6bit(a, b, part[0], __uint_as_float(e << 23));
-        part[1] = to_6bit(a, b, __uint_as_float((e - 4) << 23));  // (at most a quarter of a unit is left: 4 in units of 2^-4)
-        less_6bit(a, b, part[1], __uint_as_float((e - 4) << 23));
-        part[2] = to_6bit(a, b, __uint_as_float((e - 8) << 23));
-        uint32_t s[3] = {e, e - 4, e - 8};
-        if (top >= 0x7f800000u) s[0] = s[1] = s[2] = 255;  // not a number, and neither are the scores
-        if constexpr (DH == 64) {
-            const bool upper = lane >= 32;
-            part[0] = upper ? part[1] : part[0];
-            s[0] = upper ? s[1] : s[0];
-            part[1] = upper ? u6{} : part[2];
-            s[1] = s[2];
-        }
+        const bool bad = top >= 0x7f800000u;  // not a number, and neither are the scores
+        u6 keep = {};
+        uint32_t word = 0, kept = 0;
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            lo[rt][i][lane] = u4{part[i][0], part[i][1], part[i][2], part[i][3]};
-            hi[rt][i][lane] = u2{part[i][4], part[i][5]};
+        for (int i = 0; i < PARTS; ++i) {
+            uint32_t s = i ? e + 1 - 5 * i : e;
+            const u6 part = to_6bit(a, b, __uint_as_float(s << 23));
+            if (i + 1 < PARTS) less_6bit(a, b, part, __uint_as_float(s << 23));
+            if (bad) s = 255;
+            int at = i;
+            u6 x = part;
+            if constexpr (DH == 64) {
+                const bool upper = lane >= 32, last = i + 1 == PARTS;
+                if (i % 2 == 0) {
+                    keep = part;
+                    kept = s;
+                    if (!last) continue;
+                }
+                x = upper ? (i % 2 ? part : u6{}) : keep;
+                s = upper ? s : kept;
+                at = i / 2;
+            }
+            lo[rt][at][lane] = u4{x[0], x[1], x[2], x[3]};
+            hi[rt][at][lane] = u2{x[4], x[5]};
+            word |= s << (at % 4 * 8);
+            if (at % 4 == 3 || i + 1 == PARTS) {
+                scale[rt][at / 4][lane] = word;
+                word = 0;
+            }
         }
-        scale[rt][lane] = s[0] | s[1] << 8 | s[2] << 16;
     }
     __device__ __forceinline__ i8x get(int rt, int i, int lane) const
     {
@@ -160,13 +196,21 @@ __device__ __forceinline__ float max16(const f4 (&s)[4])
     return m;
 }
 
-template <int DH, int RT, int W>
+// Four elements of a result.
+__device__ __forceinline__ void put(bf16_t *to, const f4 &x)
+{
+    fc_store_any(to, uint2{fc_bf16_bits(x[0]) | (uint32_t)fc_bf16_bits(x[1]) << 16, fc_bf16_bits(x[2]) | (uint32_t)fc_bf16_bits(x[3]) << 16});
+}
+__device__ __forceinline__ void put(float *to, const f4 &x) { fc_store_any(to, x); }
+
+template <typename T, int DH, int RT, int W>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) void k_q4_attn(AttnArgs p)
 {
-    constexpr int DT = DH / 16, N = Queries<DH, RT>::N;
+    constexpr bool FULL = sizeof(T) == 4;
+    constexpr int DT = DH / 16, N = Queries<T, DH, RT>::N;
     static_assert(RT <= W, "a wave converts one row tile at most");
     __shared__ f4 s_o[W][RT][DT][64];
-    __shared__ Queries<DH, RT> s_q;
+    __shared__ Queries<T, DH, RT> s_q;
     __shared__ float s_ref[W][RT * 16], s_sum[W][RT * 16];
     __shared__ __align__(16) float s_start[W][64], s_f[W][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -185,14 +229,14 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
     const uint32_t bytes = (uint32_t)p.tiles * fc_q4_tile_bytes(DH);
     const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)(p.layer + (size_t)pair * bytes), 0, (int)bytes, 0x00020000);
 
-    f4 o[DT][RT];
+    f4 o[DT][RT], fine[FULL ? DT : 1][RT];
     float ref[RT], sum[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         ref[rt] = -__builtin_inff();
         sum[rt] = 0.f;
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) o[dt][rt] = f4{0.f, 0.f, 0.f, 0.f};
+        for (int dt = 0; dt < DT; ++dt) o[dt][rt] = fine[FULL ? dt : 0][rt] = f4{0.f, 0.f, 0.f, 0.f};
     }
     Tile<DH> cur;
     int t = from + wave;
@@ -202,14 +246,15 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
     }
     if (wave < RT) {
         const size_t row = min(row0 + wave * 16 + m, p.rows - 1);
-        s_q.fill(p.q + (((size_t)b * p.Hq + (size_t)j * p.g) * p.A + row) * DH + (DH == 128 ? g : g & 1) * 32, wave, lane);
+        s_q.fill((const T *)p.q + (((size_t)b * p.Hq + (size_t)j * p.g) * p.A + row) * DH + (DH == 128 ? g : g & 1) * 32, wave, lane);
     }
     __syncthreads();
     i8x q[RT][N];
-    uint32_t qs[RT];
+    uint32_t qs[RT][(N + 3) / 4];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        qs[rt] = s_q.scale[rt][lane];
+#pragma unroll
+        for (int i = 0; i < (N + 3) / 4; ++i) qs[rt][i] = s_q.scale[rt][i][lane];
 #pragma unroll
         for (int i = 0; i < N; ++i) q[rt][i] = s_q.get(rt, i, lane);
     }
@@ -221,7 +266,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
         // the sixteen rows whose weights it holds.
         {
             const float e = (float)max(cur.vs >> (lane % 4 * 8) & 255, (uint32_t)(FC_Q4_V_LOWEST + 127)) - 127.f;  // (a row never stored has 0)
-            float start = e * p.by_c, f = __builtin_amdgcn_exp2f(-e);
+            float start = FULL ? e : e * p.by_c, f = __builtin_amdgcn_exp2f(-e);
             if ((t + 1) * 64 > n) {  // rows behind the end may hold anything: weight 0, and key scales that leave scores finite
                 if (t * 64 + lane % 16 / 4 * 16 + g * 4 + lane % 4 >= n) {
                     start = -__builtin_inff();
@@ -241,20 +286,30 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
         f4 s[RT][4];
         bool move = false;
         float top[RT];
-// (part by part: products that add to one another are a latency of the matrix core apart)
-#define FC_Q4_KEYS(T, I)                                                                    \
-    _Pragma("unroll") for (int rt = 0; rt < RT; ++rt) s[rt][T] =                              \
-        multiply<T, I>(operand(cur.k[T]), cur.ks, q[rt][I], qs[rt], I == 0 ? start[T] : s[rt][T]);
+// (part by part: products that add to one another are a latency of the matrix core apart; the least first, so that they are not rounded to the
+// largest)
+#define FC_Q4_KEYS(K, I)                                                                    \
+    _Pragma("unroll") for (int rt = 0; rt < RT; ++rt) s[rt][K] =                              \
+        multiply<K, I % 4>(operand(cur.k[K]), cur.ks, q[rt][I], qs[rt][I / 4], I != FIRST ? s[rt][K] : FULL ? f4{0.f, 0.f, 0.f, 0.f} : start[K]);
 #define FC_Q4_PART(I) FC_Q4_KEYS(0, I) FC_Q4_KEYS(1, I) FC_Q4_KEYS(2, I) FC_Q4_KEYS(3, I)
-        FC_Q4_PART(0)
+        constexpr int FIRST = N - 1;
+        if constexpr (N == 6) { FC_Q4_PART(5) FC_Q4_PART(4) FC_Q4_PART(3) }
+        if constexpr (N >= 3) { FC_Q4_PART(2) }
         FC_Q4_PART(1)
-        if constexpr (N == 3) { FC_Q4_PART(2) }
+        FC_Q4_PART(0)
 #undef FC_Q4_PART
 #undef FC_Q4_KEYS
         cur.load_keys(rsrc, next, lane);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
-            top[rt] = max16(s[rt]) * p.c;
+            if constexpr (FULL) {
+                f4 x[4];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x[i / 4][i % 4] = fmaf(s[rt][i / 4][i % 4], p.c, start[i / 4][i % 4]);
+                top[rt] = max16(x);
+            } else {
+                top[rt] = max16(s[rt]) * p.c;
+            }
             move |= top[rt] > ref[rt] + MOVE;
         }
         if (__any(move)) {
@@ -263,14 +318,17 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
                 float x = top[rt];
                 x = fmaxf(x, __shfl_xor(x, 16));
                 x = fmaxf(x, __shfl_xor(x, 32));
-                const float r = fmaxf(ref[rt], x), a = __builtin_amdgcn_exp2f(ref[rt] - r);
+                const float r = fmaxf(ref[rt], FULL ? ceilf(x) : x), a = __builtin_amdgcn_exp2f(ref[rt] - r);
                 ref[rt] = r;
                 sum[rt] *= a;
 #pragma unroll
-                for (int dt = 0; dt < DT; ++dt) o[dt][rt] *= a;
+                for (int dt = 0; dt < DT; ++dt) {
+                    o[dt][rt] *= a;
+                    if constexpr (FULL) fine[dt][rt] *= a;
+                }
             }
         }
-        h8 w[RT][2];
+        h8 w[RT][2], rest[RT][2];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const f4 f = *(const f4 *)&s_f[wave][g * 16 + i * 4];
@@ -278,9 +336,10 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
             for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const float x = __builtin_amdgcn_exp2f(fmaf(s[rt][i][k], p.c, -ref[rt]));
+                    const float x = __builtin_amdgcn_exp2f(fmaf(s[rt][i][k], p.c, FULL ? start[i][k] - ref[rt] : -ref[rt]));
                     sum[rt] = fmaf(x, f[k], sum[rt]);
                     w[rt][i / 2][i % 2 * 4 + k] = (_Float16)x;
+                    if constexpr (FULL) rest[rt][i / 2][i % 2 * 4 + k] = (_Float16)((x - (float)(_Float16)x) * FINE);
                 }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -302,7 +361,10 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
                 FC_Q4_VALUES(3)
 #undef FC_Q4_VALUES
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) o[dt][rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[rt][kb], o[dt][rt], 0, 0, 0);
+                for (int rt = 0; rt < RT; ++rt) {
+                    o[dt][rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w[rt][kb], o[dt][rt], 0, 0, 0);
+                    if constexpr (FULL) fine[dt][rt] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v, rest[rt][kb], fine[dt][rt], 0, 0, 0);
+                }
             }
         cur.load_values(rsrc, next, lane);
     }
@@ -318,7 +380,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
             s_sum[wave][rt * 16 + m] = l;
         }
 #pragma unroll
-        for (int dt = 0; dt < DT; ++dt) s_o[wave][rt][dt][lane] = o[dt][rt];
+        for (int dt = 0; dt < DT; ++dt) s_o[wave][rt][dt][lane] = FULL ? o[dt][rt] + fine[FULL ? dt : 0][rt] * (1.f / FINE) : o[dt][rt];
     }
     __syncthreads();
 #pragma unroll 1
@@ -347,23 +409,19 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
         }
         const uint32_t h = p.by_a.over(row), a = row - h * p.A;
         const bool none = n == 0 || (p.pos && p.pos[(size_t)b * p.A + a] < 0);
-        const float inv = 1.f / l;
-        bf16_t *out = p.out + ((size_t)b * p.A + a) * ((size_t)p.Hq * DH) + (size_t)(j * p.g + h) * DH + dt * 16 + g * 4;
-        uint2 packed;
-        packed.x = fc_bf16_bits(none ? 0.f : x[0] * inv) | (uint32_t)fc_bf16_bits(none ? 0.f : x[1] * inv) << 16;
-        packed.y = fc_bf16_bits(none ? 0.f : x[2] * inv) | (uint32_t)fc_bf16_bits(none ? 0.f : x[3] * inv) << 16;
-        fc_store_any(out, packed);
+        T *out = (T *)p.out + ((size_t)b * p.A + a) * ((size_t)p.Hq * DH) + (size_t)(j * p.g + h) * DH + dt * 16 + g * 4;
+        put(out, none ? f4{0.f, 0.f, 0.f, 0.f} : x * (1.f / l));
     }
 }
 
 // Partial results of the ranges, added at the largest reference; a thread has four elements of a row.  Eight ranges at a time, all their loads
 // in flight together (one by one a range took 0.37 us).
-template <int DH>
+template <typename T, int DH>
 __global__ __launch_bounds__(256) void k_q4_merge(AttnArgs p)
 {
-    constexpr int T = DH / 4, N = 8;
+    constexpr int LANES = DH / 4, N = 8;
     const uint32_t pair = blockIdx.y, b = p.by_hkv.over(pair), j = pair - b * p.Hkv;
-    const int row = blockIdx.x * (256 / T) + threadIdx.x / T, d = threadIdx.x % T * 4;
+    const int row = blockIdx.x * (256 / LANES) + threadIdx.x / LANES, d = threadIdx.x % LANES * 4;
     if (row >= p.rows) return;
     const float2 *st = (const float2 *)(p.part + (size_t)p.units * p.rows * DH);
     const size_t at = (size_t)pair * p.splits * p.rows + row;
@@ -400,79 +458,23 @@ __global__ __launch_bounds__(256) void k_q4_merge(AttnArgs p)
             x += w * v[i];
         }
     }
-    const float inv = 1.f / l;
-    bf16_t *out = p.out + ((size_t)b * p.A + a) * ((size_t)p.Hq * DH) + (size_t)(j * p.g + h) * DH + d;
-    uint2 packed;
-    packed.x = fc_bf16_bits(none ? 0.f : x[0] * inv) | (uint32_t)fc_bf16_bits(none ? 0.f : x[1] * inv) << 16;
-    packed.y = fc_bf16_bits(none ? 0.f : x[2] * inv) | (uint32_t)fc_bf16_bits(none ? 0.f : x[3] * inv) << 16;
-    fc_store_any(out, packed);
+    T *out = (T *)p.out + ((size_t)b * p.A + a) * ((size_t)p.Hq * DH) + (size_t)(j * p.g + h) * DH + d;
+    put(out, none ? f4{0.f, 0.f, 0.f, 0.f} : x * (1.f / l));
 }
 
-template <int DH, int RT, int W>
+template <typename T, int DH, int RT, int W>
 void launch_w(const AttnArgs &p, hipStream_t s)
 {
     const unsigned blocks = (unsigned)((p.units + 7) / 8 * 8 * p.groups);
-    k_q4_attn<DH, RT, W><<<dim3(blocks), dim3(64 * W), 0, s>>>(p);
+    k_q4_attn<T, DH, RT, W><<<dim3(blocks), dim3(64 * W), 0, s>>>(p);
 }
-template <int DH>
+template <typename T, int DH>
 void launch(const AttnArgs &p, const FcQ4Plan &pl, hipStream_t s)
 {
-    if (pl.rt == 2) pl.waves == 8 ? launch_w<DH, 2, 8>(p, s) : launch_w<DH, 2, 4>(p, s);
-    else pl.waves == 8 ? launch_w<DH, 1, 8>(p, s) : launch_w<DH, 1, 4>(p, s);
-    if (p.splits > 1) k_q4_merge<DH><<<dim3((unsigned)((p.rows + 1024 / DH - 1) / (1024 / DH)), (unsigned)(p.units / p.splits)), dim3(256), 0, s>>>(p);
-}
-
-// One wave per query row (fp32 queries), a key per lane for the scores and an element per lane for the sums: one pass over the keys with the running
-// maximum and sum of the softmax.
-template <typename T, int DH>
-__global__ __launch_bounds__(64) void k_q4_rows(FcQ4Geom G, const T *__restrict__ q, const uint8_t *layer, const int32_t *__restrict__ pos,
-                                                const int32_t *__restrict__ lens, int A, int kv_len, T *__restrict__ out)
-{
-    __shared__ float s_q[DH], s_p[64];
-    const int lane = threadIdx.x, a = blockIdx.x, h = blockIdx.y, b = blockIdx.z;
-    const int pair = b * G.Hkv + h / G.g;
-    T *o = out + (((size_t)b * A + a) * G.Hq + h) * DH;
-    const int n = lens ? min(max(lens[b], 0), kv_len) : kv_len;
-    const bool empty = n == 0 || (pos && pos[(size_t)b * A + a] < 0);
-    constexpr int E = DH / 64;
-    float acc[E] = {}, top = -__builtin_inff(), sum = 0.f;
-    if (!empty) {
-        for (int i = lane; i < DH; i += 64) s_q[i] = fc_to_float(q[(((size_t)b * G.Hq + h) * A + a) * DH + i]) * G.scale;
-        __syncthreads();
-        for (int t0 = 0; t0 < n; t0 += FC_VTILE) {
-            const uint8_t *rec = layer + ((size_t)pair * (G.spad / FC_VTILE) + t0 / FC_VTILE) * fc_q4_tile_bytes(DH);
-            float s = 0.f;
-            for (int c = 0; c < DH / 32; ++c) {
-                const uint32_t *w = (const uint32_t *)(rec + fc_q4_k_block(DH, lane, c));
-                float part = 0.f;
-                for (int i = 0; i < 32; ++i) part += s_q[32 * c + i] * fc_q4_value(w[i / 8] >> (4 * (i % 8)) & 0xf);
-                s += part * fc_q4_scale(rec[fc_q4_kscale(DH, lane, c)]);
-            }
-            if (t0 + lane >= n) s = -__builtin_inff();
-            float m = s;
-            for (int x = 1; x < 64; x <<= 1) m = fmaxf(m, __shfl_xor(m, x));
-            const float next = fmaxf(top, m), old = expf(top - next), p = t0 + lane < n ? expf(s - next) : 0.f;
-            float l = p;
-            for (int x = 1; x < 64; x <<= 1) l += __shfl_xor(l, x);
-            sum = sum * old + l;
-            top = next;
-            __syncthreads();
-            s_p[lane] = t0 + lane < n ? p * fc_q4_scale(rec[fc_q4_vscale(DH) + fc_q4_vscale_at(lane)]) : 0.f;
-            __syncthreads();
-            const uint32_t *v = (const uint32_t *)(rec + fc_q4_v(DH));
-            for (int e = 0; e < E; ++e) {
-                const int d = 64 * e + lane;
-                acc[e] *= old;
-                for (int r0 = 0; r0 < 64; r0 += 32)
-                    for (int g = 0; g < 4; ++g) {
-                        const int w = d / 16 * 2 + r0 / 32;
-                        const uint32_t code = v[w / 4 * 256 + (g * 16 + d % 16) * 4 + w % 4];
-                        for (int j = 0; j < 8; ++j) acc[e] += s_p[r0 + j / 4 * 16 + g * 4 + j % 4] * fc_q4_value(code >> (4 * j) & 0xf);
-                    }
-            }
-        }
-    }
-    for (int e = 0; e < E; ++e) o[64 * e + lane] = fc_from_float<T>(empty ? 0.f : acc[e] / sum);
+    constexpr int RT = MOST_RT<T>;
+    if (pl.rt == 2) pl.waves == 8 ? launch_w<T, DH, RT, 8>(p, s) : launch_w<T, DH, RT, 4>(p, s);
+    else pl.waves == 8 ? launch_w<T, DH, 1, 8>(p, s) : launch_w<T, DH, 1, 4>(p, s);
+    if (p.splits > 1) k_q4_merge<T, DH><<<dim3((unsigned)((p.rows + 1024 / DH - 1) / (1024 / DH)), (unsigned)(p.units / p.splits)), dim3(256), 0, s>>>(p);
 }
 
 }  // namespace
@@ -528,13 +530,14 @@ FcQ4Plan plan(const FcQ4Geom &G, int A, int kv_len, size_t cap)
     FcQ4Plan best{1, 4, 1};
     const FcKnobs &k = fc_knobs();
     if (k.q4_rt > 0) {  // a tuning knob asks for one
-        best = FcQ4Plan{k.q4_rt == 2 ? 2 : 1, k.q4_waves == 8 ? 8 : 4, k.q4_splits > 0 ? k.q4_splits : 1};
+        best = FcQ4Plan{k.q4_rt == 2 && G.dtype != FC_F32 ? 2 : 1, k.q4_waves == 8 ? 8 : 4, k.q4_splits > 0 ? k.q4_splits : 1};
         if (best.splits > tiles) best.splits = (int)tiles;
         while (best.splits > 1 && fc_q4_plan_workspace(G, best, A) > cap) --best.splits;
         return best;
     }
     double least = 1e30;
     for (const Q4Shape &sh : G.Dh == 128 ? Q4_128 : Q4_64) {
+        if (sh.rt == 2 && G.dtype == FC_F32) continue;
         const int64_t groups = (rows + 16 * sh.rt - 1) / (16 * sh.rt);
         for (const int splits : SPLITS) {
             const FcQ4Plan pl{sh.rt, sh.waves, splits};
@@ -554,25 +557,24 @@ FcQ4Plan plan(const FcQ4Geom &G, int A, int kv_len, size_t cap)
 // Upper bound of what a plan for up to max_rows rows uses: 64 ranges of every row, or 512 workgroups of 32 rows.
 size_t fc_q4_most_workspace(const FcQ4Geom &G, int max_rows)
 {
-    if (G.dtype == FC_F32 || G.spad <= FC_VTILE) return 0;
+    if (G.spad <= FC_VTILE) return 0;
     const int64_t rows = (int64_t)G.B * G.Hkv * G.g * max_rows * MOST_SPLITS, most = (int64_t)MOST_WGS * 32;
     return (size_t)(rows < most ? rows : most) * (G.Dh + 2) * sizeof(float);
 }
 
 FcQ4Plan fc_plan_q4(const FcQ4Geom &G, int A, int kv_len, size_t cap)
 {
-    if (G.dtype == FC_F32) return FcQ4Plan{1, 4, 1};
     const size_t most = fc_q4_most_workspace(G, A);
     if (cap > most && !fc_knobs().q4_rt) cap = most;  // (more changes nothing)
     // The last few plans of this thread: a program calls with one shape for every layer.
     struct Entry {
-        int key[7];
+        int key[8];
         size_t cap;
         FcQ4Plan plan;
     };
     static thread_local Entry known[4];
     static thread_local unsigned next = 0;
-    const int key[7] = {G.B, G.Hkv, G.g, G.Dh, A, kv_len, fc_knobs().version + 1};
+    const int key[8] = {G.B, G.Hkv, G.g, G.Dh, G.dtype, A, kv_len, fc_knobs().version + 1};
     for (const Entry &e : known)
         if (e.cap == cap && !memcmp(e.key, key, sizeof key)) return e.plan;
     Entry &e = known[next++ % 4];
@@ -584,18 +586,12 @@ FcQ4Plan fc_plan_q4(const FcQ4Geom &G, int A, int kv_len, size_t cap)
 hipError_t fc_launch_q4_attention(const FcQ4Geom &G, const FcQ4Plan &pl, const void *q, const uint8_t *layer, const int32_t *pos, const int32_t *lens,
                                   int A, int kv_len, void *out, void *workspace, hipStream_t s)
 {
-    if (G.dtype == FC_F32) {
-        const dim3 grid((unsigned)A, (unsigned)G.Hq, (unsigned)G.B);
-        if (G.Dh == 128) k_q4_rows<float, 128><<<grid, dim3(64), 0, s>>>(G, (const float *)q, layer, pos, lens, A, kv_len, (float *)out);
-        else k_q4_rows<float, 64><<<grid, dim3(64), 0, s>>>(G, (const float *)q, layer, pos, lens, A, kv_len, (float *)out);
-        return hipGetLastError();
-    }
     AttnArgs p;
-    p.q = (const bf16_t *)q;
+    p.q = q;
     p.layer = layer;
     p.pos = pos;
     p.lens = lens;
-    p.out = (bf16_t *)out;
+    p.out = out;
     p.part = (float *)workspace;
     p.A = A;
     p.kv_len = kv_len;
@@ -613,7 +609,7 @@ hipError_t fc_launch_q4_attention(const FcQ4Geom &G, const FcQ4Plan &pl, const v
     p.by_splits.set((uint32_t)p.splits);
     p.by_hkv.set((uint32_t)p.Hkv);
     p.by_a.set((uint32_t)A);
-    if (G.Dh == 128) launch<128>(p, pl, s);
-    else launch<64>(p, pl, s);
+    if (G.dtype == FC_F32) G.Dh == 128 ? launch<float, 128>(p, pl, s) : launch<float, 64>(p, pl, s);
+    else G.Dh == 128 ? launch<bf16_t, 128>(p, pl, s) : launch<bf16_t, 64>(p, pl, s);
     return hipGetLastError();
 }
