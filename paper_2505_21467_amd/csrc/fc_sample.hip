@@ -22,14 +22,36 @@
 namespace {
 
 constexpr int BINS = 1024, PER_T = 32;       // bins; bins to a unit of z / T
-constexpr int SCAN = 512, PART = 16384;      // threads, and entries of a part: its counts fit 15 bits, its sums 47
+constexpr int SCAN = 512;                    // threads of a part of a row
+constexpr int SHORT = 4096, LONG = 16384;    // its entries, at least and at most: their count fits 15 bits, their sum 47
 constexpr int PICK = 1024;                   // threads of the second kernel, one to a bin
 constexpr int CAP = 12288;                   // entries that it fetches into LDS
 constexpr int LISTED = 256, LIST = 1024;     // entries that a part lists, about, and at most
 constexpr int FEW = 64;                      // entries that one wave compares with one another
 constexpr int SUM_BITS = 48;
 
-__host__ __device__ inline int parts_of(int V) { return (V + PART - 1) / PART; }
+// exp(-i) and exp(-i / 32): a bin's factor is a product of two.  (The library's function costs 2 us here, most of it for code that is not in the
+// instruction cache.)
+struct Factors {
+    double whole[BINS / PER_T], part[PER_T];
+};
+constexpr Factors factors()
+{
+    const double power[5] = {0.36787944117144233, 0.1353352832366127, 0.01831563888873418, 0.00033546262790251185, 1.1253517471925912e-07};  // exp(-2^i)
+    Factors f{};
+    for (int i = 0; i < BINS / PER_T; ++i) {
+        f.whole[i] = 1.;
+        for (int k = 0; k < 5; ++k)
+            if (i >> k & 1) f.whole[i] *= power[k];
+    }
+    for (int i = 0; i < PER_T; ++i) {
+        double term = 1.;
+        for (int k = 1; k < 20; ++k) f.part[i] += term, term *= -(double)i / (PER_T * k);
+    }
+    return f;
+}
+static_assert(BINS / PER_T == 32, "five powers");
+__constant__ const Factors FACTORS = factors();
 
 // Order of the entries as a number: the larger logit first, then the smaller index.  -0 is 0.
 __device__ __forceinline__ uint64_t rank_of(float z, uint32_t index)
@@ -51,6 +73,7 @@ struct Grid {
     __device__ __forceinline__ Grid(float most_, double c_) : most(most_), infinite(most_ > 3.4028235e38f), c(c_), top(floor((double)most_ * c_)) {}
     __device__ __forceinline__ int bin(float z, double &within) const
     {
+#pragma clang fp contract(off)  // (x is rounded: with one fused operation for x - b an entry's weight would depend on where it is computed)
         const double x = (double)z * c, b = floor(x);
         within = x - b;
         const double d = top - b;
@@ -81,16 +104,32 @@ struct Grid {
 // 16 bytes of a row.
 template <typename T>
 struct Piece {
-    static constexpr int N = 16 / sizeof(T);
+    static constexpr int N = 16 / sizeof(T), BITS = 8 * sizeof(T);
     T v[N];
-    __device__ __forceinline__ void load(const T *z, int at, int n)  // -inf from n on
+    // Entries at .. of a row, -inf from `end` on.  A piece that is not whole is the last 16 bytes shifted (a row of fewer: one by one).
+    __device__ __forceinline__ void load(const T *z, int at, int end)
     {
-        if (at + N <= n) *this = __builtin_bit_cast(Piece, fc_load_any<uint4>(z + at));
-        else
+        const int back = min(max(at + N - end, 0), N);
+        if (end >= N) *this = __builtin_bit_cast(Piece, fc_load_any<uint4>(z + min(at, end - N)));
+        if (back == 0) return;
+        if (end < N) {
 #pragma unroll
-            for (int j = 0; j < N; ++j) v[j] = at + j < n ? z[at + j] : fc_from_float<T>(-__builtin_inff());
+            for (int j = 0; j < N; ++j) v[j] = at + j < end ? z[at + j] : fc_from_float<T>(-__builtin_inff());
+            return;
+        }
+        const unsigned __int128 least = (unsigned __int128)LEAST << 64 | LEAST;
+        if (back == N) *this = __builtin_bit_cast(Piece, least);
+        else *this = __builtin_bit_cast(Piece, __builtin_bit_cast(unsigned __int128, *this) >> (back * BITS) | least << ((N - back) * BITS));
     }
     __device__ __forceinline__ float get(int j) const { return fc_to_float(v[j]); }
+    __device__ __forceinline__ float at(int j) const  // (any j: a shift, not an index)
+    {
+        struct halves { uint64_t v[2]; };
+        const halves h = __builtin_bit_cast(halves, *this);
+        const uint32_t x = (uint32_t)((j < N / 2 ? h.v[0] : h.v[1]) >> (j % (N / 2) * BITS));
+        return sizeof(T) == 2 ? __uint_as_float(x << 16) : __uint_as_float(x);
+    }
+    static constexpr uint64_t LEAST = sizeof(T) == 2 ? 0xff80ff80ff80ff80ull : 0xff800000ff800000ull;
 };
 
 // Every entry of a row's first n: f(index, logit).
@@ -107,16 +146,31 @@ __device__ __forceinline__ void each_entry(const T *z, int n, F f)
     }
 }
 
-// Inclusive running sum over a wave.
+// The value of the lane that CTRL names, 0 where there is none or the row of 16 lanes is not in ROWS.
+template <int CTRL, int ROWS, typename X>
+__device__ __forceinline__ X from_lane(X x)
+{
+    struct words { int v[sizeof(X) / 4]; };
+    words w = __builtin_bit_cast(words, x);
+#pragma unroll
+    for (int &v : w.v) v = __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+    return __builtin_bit_cast(X, w);
+}
+// Running results over a wave: one, two, four, eight lanes before within a row of 16, the last lane of the row before, of the half before.
+template <typename X, typename F>
+__device__ __forceinline__ X wave_run(X x, F f)
+{
+    x = f(x, from_lane<0x111, 0xf>(x));
+    x = f(x, from_lane<0x112, 0xf>(x));
+    x = f(x, from_lane<0x114, 0xf>(x));
+    x = f(x, from_lane<0x118, 0xf>(x));
+    x = f(x, from_lane<0x142, 0xa>(x));
+    return f(x, from_lane<0x143, 0xc>(x));
+}
 template <typename X>
 __device__ __forceinline__ X wave_scan(X x)
 {
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const X y = __shfl_up(x, o);
-        if ((threadIdx.x & 63) >= (unsigned)o) x += y;
-    }
-    return x;
+    return wave_run(x, [](X a, X b) { return a + b; });
 }
 
 // What is kept of a part besides its bins: the largest logit; the last bin of which the list has every entry (-1: none); their number.
@@ -130,25 +184,25 @@ struct Part {
 //
 // The largest entries of the threads' pieces say where to end: at least as many entries as pieces reach a bin, so with a top-k nothing below the
 // bin that k pieces reach can be kept, and is not weighed; the list ends at the bin that 256 reach.
-template <typename T>
+template <typename T, int PART>
 __global__ __launch_bounds__(SCAN) void k_sample_bins(FcSampleArgs p, int parts, uint64_t *__restrict__ bins, uint64_t *__restrict__ list,
-                                                      Part *__restrict__ about)
+                                                      Part *__restrict__ about, unsigned long long *__restrict__ shared)
 {
-    constexpr int N = Piece<T>::N, PIECES = PART / (SCAN * N), U = PIECES / 4;  // (U pieces are eight values)
+    constexpr int N = Piece<T>::N, PIECES = PART / (SCAN * N);  // (U pieces are eight values)
     __shared__ unsigned long long s_bin[BINS];
-    __shared__ uint32_t s_count[BINS], s_wave[SCAN / 64], s_n;
+    __shared__ uint32_t s_count[BINS], s_wave[SCAN / 64], s_n, s_pieces;
     __shared__ float s_max[SCAN / 64];
     __shared__ int s_last[2];
-    __shared__ uint64_t s_queue[SCAN / 64][64 + 8 * 64];
+    __shared__ uint16_t s_piece[PIECES * SCAN];
     const int tid = threadIdx.x;
     const uint32_t row = blockIdx.x / (uint32_t)parts, part = blockIdx.x - row * parts;
-    const int from = part * PART, n = min(p.V - from, PART);
-    const T *z = (const T *)p.logits + (size_t)row * p.ld + from;
+    const int from = part * PART, to = min(p.V, from + PART);
+    const T *z = (const T *)p.logits + (size_t)row * p.ld;
     const size_t at = (size_t)row * parts + part;
     Piece<T> x[PIECES];
     float best[PIECES];
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) x[i].load(z, (i * SCAN + tid) * N, n);
+    for (int i = 0; i < PIECES; ++i) x[i].load(z, from + (i * SCAN + tid) * N, to);
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
         best[i] = -__builtin_inff();
@@ -167,7 +221,7 @@ __global__ __launch_bounds__(SCAN) void k_sample_bins(FcSampleArgs p, int parts,
     }
     if (tid == 0) {
         s_last[0] = s_last[1] = BINS;
-        s_n = 0;
+        s_n = s_pieces = 0;
     }
     __syncthreads();
 #pragma unroll
@@ -196,63 +250,45 @@ __global__ __launch_bounds__(SCAN) void k_sample_bins(FcSampleArgs p, int parts,
         const int last = min(min(p.last_bin, BINS - 1), s_last[0] + 2);
         end = min(last, s_last[1] + 2);
         const float cut = g.lowest(last);
-        // Eight values a turn, then the pieces move up: short code, and registers that no index picks.  Where most lanes have nothing that matters,
-        // entries pass through a queue of the wave's, so that all its lanes weigh: under a top-k of 50 one entry in hundreds does (32 x 152064
-        // bf16: 30 us with the queue, 48 without), with none at temperature 1 all do (33 x 32001 fp32: 18 us with it, 13.5 without).
-        uint64_t *queue = s_queue[tid / 64];
-        uint32_t held = 0;
-        auto weigh = [&](float v, int i) {
-            double within;
-            const int bin = g.bin(v, within);
-            if (bin > last) return;
-            atomicAdd(&s_bin[bin], (unsigned long long)(1ull << SUM_BITS | g.weight(within)));
-            if (bin > end) return;
-            const uint32_t to = atomicAdd(&s_n, 1u);
-            if (to < LIST) list[at * LIST + to] = rank_of(v, (uint32_t)(from + i));
-        };
+        // Pieces with an entry that matters are listed, spread over the threads and read again: under a top-k of 50 one entry in hundreds does, and every
+        // wave has some.
+#pragma unroll
+        for (int i = 0; i < PIECES; ++i) {
+            const uint64_t in = __ballot(best[i] >= cut);
+            if (!in) continue;
+            uint32_t base = 0;
+            if (tid % 64 == 0) base = atomicAdd(&s_pieces, (uint32_t)__builtin_popcountll(in));
+            base = __builtin_amdgcn_readfirstlane(base);
+            const uint32_t to = __builtin_amdgcn_mbcnt_hi((uint32_t)(in >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in, base));
+            if (best[i] >= cut) s_piece[to] = (uint16_t)(i * SCAN + tid);
+        }
+        __syncthreads();
 #pragma unroll 1
-        for (int i = 0; i < PIECES; i += U) {
-            int in = 0;
+        for (int i = tid; i < (int)s_pieces; i += SCAN) {
+            const int first = from + s_piece[i] * N;
+            Piece<T> x;
+            x.load(z, first, to);
+            uint32_t in = 0;
 #pragma unroll
-            for (int k = 0; k < U; ++k)
-#pragma unroll
-                for (int j = 0; j < N; ++j) in += __builtin_popcountll(__ballot(x[k].get(j) >= cut));
-            if (in >= 64 * U * N / 2) {
-#pragma unroll
-                for (int k = 0; k < U; ++k)
-#pragma unroll
-                    for (int j = 0; j < N; ++j)
-                        if (x[k].get(j) >= cut) weigh(x[k].get(j), ((i + k) * SCAN + tid) * N + j);
-            } else if (in) {
-#pragma unroll
-                for (int k = 0; k < U; ++k)
-#pragma unroll
-                    for (int j = 0; j < N; ++j) {
-                        const float v = x[k].get(j);
-                        const uint64_t mask = __ballot(v >= cut);
-                        const uint32_t to = __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, held));
-                        if (v >= cut) queue[to] = (uint64_t)__float_as_uint(v) << 32 | (uint32_t)(((i + k) * SCAN + tid) * N + j);
-                        held += (uint32_t)__builtin_popcountll(mask);
-                    }
-            }
-#pragma unroll
-            for (int k = 0; k + U < PIECES; ++k) x[k] = x[k + U];
-            const bool more = i + U < PIECES;
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            for (int j = 0; j < N; ++j) in |= x.get(j) >= cut ? 1u << j : 0;
 #pragma unroll 1
-            while (held >= 64 || (!more && held)) {
-                const uint32_t n = min(held, 64u);
-                held -= n;
-                if ((uint32_t)(tid % 64) < n) {
-                    const uint64_t e = queue[held + tid % 64];
-                    weigh(__uint_as_float((uint32_t)(e >> 32)), (int)(uint32_t)e);
-                }
+            while (in) {
+                const int j = __builtin_ctz(in);
+                in &= in - 1;
+                const float v = x.at(j);
+                double within;
+                const int bin = g.bin(v, within);
+                if (bin > last) continue;
+                atomicAdd(&s_bin[bin], (unsigned long long)(1ull << SUM_BITS | g.weight(within)));
+                if (bin > end) continue;
+                const uint32_t place = atomicAdd(&s_n, 1u);
+                if (place < LIST) list[at * LIST + place] = rank_of(v, (uint32_t)(first + j));
             }
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         }
     }
     __syncthreads();
     for (int i = tid; i < BINS; i += SCAN) bins[at * BINS + i] = s_bin[i];
+    if (tid == 0 && part == 0) shared[row] = 0;
     if (tid == 0) about[at] = Part{top, s_n <= LIST ? end : -1, min(s_n, (uint32_t)LIST)};
 }
 
@@ -266,12 +302,13 @@ struct PickShared {
     uint32_t count[BINS];   // running counts
     uint64_t sum[BINS];     // the bins' own sums
     uint64_t list[CAP];     // ranks
+    uint64_t own[PICK];
     double wave_sum[PICK / 64];
     uint32_t wave_count[PICK / 64];
     uint64_t digit_sum[256];
     uint32_t digit_count[256];
     Entry few[FEW];
-    unsigned long long low, high, sum_found, rank_found, weight_found;
+    unsigned long long ones, zeros, shared, sum_found, rank_found, weight_found;
     uint32_t n, digit, count_found;
 };
 
@@ -279,10 +316,25 @@ struct Found {
     uint64_t rank, sum, weight;  // the entry, the weight of all up to it, its own
 };
 
-// Among the n entries that each(f) calls f(rank, weight) for: the one at which the running count (COUNT) or sum, larger ranks first, passes
+// Of n entries, one a lane: number and weight of those before this lane's.
+__device__ __forceinline__ uint64_t of_lane(uint64_t x, uint32_t lane)
+{
+    return (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), (int)lane) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x, (int)lane);
+}
+__device__ __forceinline__ void before_own(const Entry &own, uint32_t n, uint64_t &weight, uint32_t &count)
+{
+#pragma unroll 4
+    for (uint32_t i = 0; i < n; ++i) {
+        const uint64_t rank = of_lane(own.rank, i), w = of_lane(own.weight, i);
+        weight += rank > own.rank ? w : 0;
+        count += rank > own.rank;
+    }
+}
+
+// Among the n entries that each(f) calls f(rank, weight) for: the one at which the running count or sum, larger ranks first, passes
 // `target`; the last one if none does.  Digits of 8 bits from the first bit in which the ranks differ, until a wave can compare what is left.
-template <bool COUNT, typename EACH>
-__device__ Found select(PickShared &s, uint32_t n, uint64_t target, EACH each)
+template <typename EACH>
+__device__ Found select(PickShared &s, bool counting, uint32_t n, uint64_t target, EACH each)
 {
     const int tid = threadIdx.x;
     uint64_t low = 0, high = ~0ull, sum = 0;
@@ -291,31 +343,28 @@ __device__ Found select(PickShared &s, uint32_t n, uint64_t target, EACH each)
     while (n > FEW) {
         __syncthreads();
         if (tid == 0) {
-            s.low = ~0ull;
-            s.high = 0;
+            s.ones = s.zeros = 0;
         }
         if (tid < 256) {
             s.digit_sum[tid] = 0;
             s.digit_count[tid] = 0;
         }
         __syncthreads();
-        uint64_t a = ~0ull, b = 0;
+        uint64_t ones = 0, zeros = 0;
         each([&](uint64_t rank, uint64_t) {
             if (rank < low || rank > high) return;
-            a = min(a, rank);
-            b = max(b, rank);
+            ones |= rank;
+            zeros |= ~rank;
         });
-#pragma unroll 1
-        for (int o = 1; o < 64; o <<= 1) {
-            a = min(a, (uint64_t)__shfl_xor((unsigned long long)a, o));
-            b = max(b, (uint64_t)__shfl_xor((unsigned long long)b, o));
-        }
-        if (a <= b && tid % 64 == 0) {
-            atomicMin(&s.low, (unsigned long long)a);
-            atomicMax(&s.high, (unsigned long long)b);
+        auto either = [](uint64_t x, uint64_t y) { return x | y; };
+        ones = wave_run(ones, either);
+        zeros = wave_run(zeros, either);
+        if (tid % 64 == 63 && ones) {
+            atomicOr(&s.ones, (unsigned long long)ones);
+            atomicOr(&s.zeros, (unsigned long long)zeros);
         }
         __syncthreads();
-        const int bits = 64 - __builtin_clzll(s.low ^ s.high), shift = bits > 8 ? bits - 8 : 0;
+        const int bits = 64 - __builtin_clzll(s.ones & s.zeros), shift = bits > 8 ? bits - 8 : 0;
         const uint32_t mask = (uint32_t)((bits - shift < 8 ? 1u << (bits - shift) : 256u) - 1);
         each([&](uint64_t rank, uint64_t w) {
             if (rank < low || rank > high) return;
@@ -333,7 +382,7 @@ __device__ Found select(PickShared &s, uint32_t n, uint64_t target, EACH each)
             }
             unsigned long long run = sum + wave_scan(own);
             uint32_t runs = count + wave_scan(owns);
-            const uint64_t passed = __ballot(COUNT ? runs > target : run > target), some = __ballot(owns > 0);
+            const uint64_t passed = __ballot(counting ? runs > target : run > target), some = __ballot(owns > 0);
             const int lane = passed ? __builtin_ctzll(passed) : 63 - __builtin_clzll(some);  // (none: the last one with entries)
             if (tid == lane) {
                 run -= own;
@@ -342,7 +391,7 @@ __device__ Found select(PickShared &s, uint32_t n, uint64_t target, EACH each)
                 for (int i = 0; i < 4; ++i, --d) {
                     if (!s.digit_count[d]) continue;
                     last = d;
-                    if (COUNT ? runs + s.digit_count[d] > target : run + s.digit_sum[d] > target) break;
+                    if (counting ? runs + s.digit_count[d] > target : run + s.digit_sum[d] > target) break;
                     run += s.digit_sum[d];
                     runs += s.digit_count[d];
                 }
@@ -359,7 +408,7 @@ __device__ Found select(PickShared &s, uint32_t n, uint64_t target, EACH each)
         sum = s.sum_found;
         count = s.count_found;
         n = s.digit_count[s.digit];
-        low = (bits < 64 ? s.low >> bits << bits : 0) | (uint64_t)s.digit << shift;
+        low = (bits < 64 ? s.ones >> bits << bits : 0) | (uint64_t)s.digit << shift;
         high = low | ((1ull << shift) - 1);
     }
     __syncthreads();
@@ -372,18 +421,14 @@ __device__ Found select(PickShared &s, uint32_t n, uint64_t target, EACH each)
     });
     __syncthreads();
     n = min(s.n, (uint32_t)FEW);
-    if (tid < (int)n) {
+    if (tid < 64) {
         const Entry own = s.few[tid];
         uint64_t run = sum;
         uint32_t runs = 0;
-        for (uint32_t i = 0; i < n; ++i)
-            if (s.few[i].rank > own.rank) {
-                run += s.few[i].weight;
-                ++runs;
-            }
-        const bool passes = COUNT ? count + runs + 1 > target : run + own.weight > target;
-        const bool before = COUNT ? count + runs > target : run > target;
-        if ((passes && !before) || (!passes && runs == n - 1)) {
+        before_own(own, n, run, runs);
+        const bool passes = counting ? count + runs + 1 > target : run + own.weight > target;
+        const bool before = counting ? count + runs > target : run > target;
+        if ((uint32_t)tid < n && ((passes && !before) || (!passes && runs == n - 1))) {
             s.rank_found = own.rank;
             s.sum_found = run + own.weight;
             s.weight_found = own.weight;
@@ -394,8 +439,7 @@ __device__ Found select(PickShared &s, uint32_t n, uint64_t target, EACH each)
 }
 
 // What select() finds, in one wave without a barrier: entries of bin b in the list, FEW at most.
-template <bool COUNT>
-__device__ __attribute__((noinline)) Found select_few(PickShared &s, const Grid &g, int listed, int b, uint64_t target)
+__device__ __attribute__((noinline)) Found select_few(PickShared &s, bool counting, const Grid &g, int listed, int b, uint64_t target)
 {
     const int lane = threadIdx.x;
     const float low = g.lowest(b), high = g.highest(b);
@@ -416,28 +460,47 @@ __device__ __attribute__((noinline)) Found select_few(PickShared &s, const Grid 
     const Entry own = s.few[lane];
     uint64_t run = 0;
     uint32_t runs = 0;
-#pragma unroll 1
-    for (uint32_t i = 0; i < n; ++i) {
-        const Entry e = s.few[i];
-        if (e.rank > own.rank) {
-            run += e.weight;
-            ++runs;
-        }
-    }
+    before_own(own, n, run, runs);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     const uint64_t to = run + own.weight;
-    const bool passes = COUNT ? runs + 1 > target : to > target, before = COUNT ? runs > target : run > target;
+    const bool passes = counting ? runs + 1 > target : to > target, before = counting ? runs > target : run > target;
     const uint64_t mask = __ballot((uint32_t)lane < n && ((passes && !before) || (!passes && runs == n - 1)));
     const int at = mask ? __builtin_ctzll(mask) : 0;
     return Found{(uint64_t)__shfl((unsigned long long)own.rank, at), (uint64_t)__shfl((unsigned long long)to, at), (uint64_t)__shfl((unsigned long long)own.weight, at)};
 }
 
-// The entries of bin b, n of them, in the list or (LIST false) in the row.
-template <typename T, bool LIST, bool COUNT>
-__device__ __attribute__((noinline)) Found select_in(PickShared &s, const T *z, int V, const Grid &g, int listed, int b, uint32_t n, uint64_t target)
+// The entries of bin b in the list, PICK at most: one a thread.
+__device__ __attribute__((noinline)) Found select_one_each(PickShared &s, bool counting, const Grid &g, int listed, int b, uint64_t target)
 {
     const float low = g.lowest(b), high = g.highest(b);
-    return select<COUNT>(s, n, target, [&](auto f) {
+    double within;
+    __syncthreads();
+    if (threadIdx.x == 0) s.n = 0;
+    __syncthreads();
+#pragma unroll 1
+    for (int i = threadIdx.x; i < listed; i += PICK) {
+        const uint64_t rank = s.list[i];
+        const float x = logit_of(rank);
+        if (!(x >= low && x <= high && g.bin(x, within) == b)) continue;
+        const uint32_t at = atomicAdd(&s.n, 1u);
+        if (at < PICK) s.own[at] = rank;
+    }
+    __syncthreads();
+    const uint32_t n = min(s.n, (uint32_t)PICK);
+    const uint64_t rank = s.own[threadIdx.x];
+    g.bin(logit_of(rank), within);
+    const uint64_t weight = g.weight(within);
+    return select(s, counting, n, target, [&](auto f) {
+        if (threadIdx.x < n) f(rank, weight);
+    });
+}
+
+// The entries of bin b, n of them, in the list or (LIST false) in the row.
+template <typename T, bool LIST>
+__device__ __attribute__((noinline)) Found select_in(PickShared &s, bool counting, const T *z, int V, const Grid &g, int listed, int b, uint32_t n, uint64_t target)
+{
+    const float low = g.lowest(b), high = g.highest(b);
+    return select(s, counting, n, target, [&](auto f) {
         double within;
         if constexpr (LIST) {
 #pragma unroll 1
@@ -454,22 +517,58 @@ __device__ __attribute__((noinline)) Found select_in(PickShared &s, const T *z, 
     });
 }
 
+// Entries [from, to) of a row with logits in one of n ranges: to the list, as far as there is room.  64 values of a thread are in flight together;
+// the few that are wanted are read again.
+template <typename T>
+__device__ __attribute__((noinline)) void fetch(PickShared &s, const T *z, int from, int to, int n, float least0, float most0, float least1, float most1,
+                                                float least2, float most2)
+{
+    constexpr int N = Piece<T>::N, U = 64 / N;
+    if (to < N) {  // a row of a few entries
+        if ((int)threadIdx.x < to) s.list[atomicAdd(&s.n, 1u)] = rank_of(fc_to_float(z[threadIdx.x]), threadIdx.x);
+        return;
+    }
+#pragma unroll 1
+    for (int i0 = from + threadIdx.x * N; i0 < to; i0 += U * PICK * N) {
+        Piece<T> x[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) x[k] = __builtin_bit_cast(Piece<T>, fc_load_any<uint4>(z + min(i0 + k * PICK * N, to - N)));
+        uint32_t in[2] = {};
+#pragma unroll 1
+        for (int r = 0; r < n; ++r) {
+            const float least = r == 0 ? least0 : r == 1 ? least1 : least2, most = r == 0 ? most0 : r == 1 ? most1 : most2;
+#pragma unroll
+            for (int k = 0; k < U * N; ++k) in[k / 32] |= x[k / N].get(k % N) >= least && x[k / N].get(k % N) <= most ? 1u << (k % 32) : 0;
+        }
+        uint64_t left = (uint64_t)in[1] << 32 | in[0];
+#pragma unroll 1
+        while (left) {
+            const int k = __builtin_ctzll(left), i1 = i0 + k / N * (PICK * N), i = min(i1, to - N) + k % N;
+            left &= left - 1;
+            if (i < i1) continue;  // (of the last 16 bytes, what another piece has)
+            const uint32_t at = atomicAdd(&s.n, 1u);
+            if (at < CAP) s.list[at] = rank_of(fc_to_float(z[i]), (uint32_t)i);
+        }
+    }
+}
+
 template <typename T>
 __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts, const uint64_t *__restrict__ bins, const uint64_t *__restrict__ lists,
-                                                      const Part *__restrict__ abouts)
+                                                      const Part *__restrict__ abouts, unsigned long long *shared, uint64_t *fetched)
 {
     __shared__ PickShared s;
-    const int tid = threadIdx.x, row = blockIdx.x;
+    const int tid = threadIdx.x, row = blockIdx.x, slices = gridDim.y, slice = blockIdx.y;
     const T *z = (const T *)p.logits + (size_t)row * p.ld;
     const Part *about = abouts + (size_t)row * parts;
     const uint64_t *part = bins + (size_t)row * parts * BINS, *lst = lists + (size_t)row * parts * LIST;
 
+    const double factor = FACTORS.whole[tid / PER_T] * FACTORS.part[tid % PER_T];
     float z_max = -__builtin_inff();
     for (int i = tid % 64; i < parts; i += 64) z_max = fmaxf(z_max, about[i].largest);
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) z_max = fmaxf(z_max, __shfl_xor(z_max, o));
     if (z_max == -__builtin_inff()) {
-        if (tid == 0) {
+        if (tid == 0 && slice == 0) {
             p.tok[row] = -1;
             p.conf[row] = 0.f;
         }
@@ -509,7 +608,6 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
     }
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) lists_to = min(lists_to, __shfl_xor(lists_to, o));
-    const double factor = exp(-(double)tid / PER_T);
     double cum = wave_scan((double)sum * factor);
     uint32_t counts = wave_scan(count);
     if (tid % 64 == 63) {
@@ -581,11 +679,11 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
     const float flow = apart && f1 >= 0 ? g.lowest(f1) : none, fhigh = apart && f1 >= 0 ? g.highest(f0) : -none;
     const float klow = apart && kb < BINS ? g.lowest(kb) : none, khigh = apart && kb < BINS ? g.highest(kb) : -none;
     auto wanted = [&](float x) { return (x >= slow && x <= shigh) || (apart && ((x >= flow && x <= fhigh) || (x >= klow && x <= khigh))); };
-    auto take = [&](uint64_t rank) {
-        const uint32_t to = atomicAdd(&s.n, 1u);
-        if (to < CAP) s.list[to] = rank;
-    };
+    auto within = [&](int b0, int b1) { return b0 <= b1 && b1 < BINS ? s.count[b1] - counted(b0) : 0u; };
+    // (too many for the list: bin by bin, then)
+    const bool by_bin = (apart ? within(sb0, sb1) + within(f0, f1) + within(kb, kb) : within(first, final)) > (uint32_t)CAP;
     if (final <= lists_to) {  // a wave to a part
+        if (slice) return;
 #pragma unroll 1
         for (int i = tid / 64; i < parts; i += PICK / 64) {
             const uint32_t n = about[i].n;
@@ -596,59 +694,74 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
                 for (int k = 0; k < 4; ++k) r[k] = lst[(size_t)i * LIST + min(j0 + k * 64, n - 1)];
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
-                    if (j0 + k * 64 < n && wanted(logit_of(r[k]))) take(r[k]);
+                    if (j0 + k * 64 < n && wanted(logit_of(r[k]))) {
+                        const uint32_t to = atomicAdd(&s.n, 1u);
+                        if (to < CAP) s.list[to] = r[k];
+                    }
             }
         }
-    } else {  // eight pieces of a thread in flight together
-        constexpr int N = Piece<T>::N, U = 8;
-#pragma unroll 1
-        for (int i0 = tid * N; i0 < p.V; i0 += U * PICK * N) {
-            Piece<T> x[U];
-#pragma unroll
-            for (int k = 0; k < U; ++k) x[k].load(z, i0 + k * PICK * N, p.V);
-            if (apart) {
-#pragma unroll
-                for (int k = 0; k < U; ++k)
-#pragma unroll
-                    for (int j = 0; j < N; ++j)
-                        if (wanted(x[k].get(j))) take(rank_of(x[k].get(j), (uint32_t)(i0 + k * PICK * N + j)));
-            } else {
-#pragma unroll
-                for (int k = 0; k < U; ++k)
-#pragma unroll
-                    for (int j = 0; j < N; ++j)
-                        if (x[k].get(j) >= slow && x[k].get(j) <= shigh) take(rank_of(x[k].get(j), (uint32_t)(i0 + k * PICK * N + j)));
-            }
+    } else if (by_bin) {
+        if (slice) return;
+    } else {
+        const int per = ((p.V + slices - 1) / slices + 7) / 8 * 8;
+        fetch(s, z, slice * per, min(p.V, (slice + 1) * per), apart ? 3 : 1, slow, shigh, flow, fhigh, klow, khigh);
+        if (slices > 1) {  // the last one to come finds what all have fetched
+            __syncthreads();
+            const uint32_t own = s.n;
+            if (tid == 0) s.shared = atomicAdd(&shared[row], (unsigned long long)own);
+            __syncthreads();
+            // (Agent-scope stores and loads go past the dies' caches, and a ticket is drawn when the stores have arrived: a fence would write
+            // back a whole cache, which took 60 us.)
+            uint64_t *of_all = fetched + (size_t)row * CAP;
+            const uint32_t at = (uint32_t)s.shared;
+            for (uint32_t i = tid; i < own && at + i < (uint32_t)CAP; i += PICK)
+                __hip_atomic_store(&of_all[at + i], s.list[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __builtin_amdgcn_s_waitcnt(0);
+            __syncthreads();
+            if (tid == 0) s.shared = atomicAdd(&shared[row], 1ull << 32);
+            __syncthreads();
+            if ((uint32_t)(s.shared >> 32) + 1 != (uint32_t)slices) return;
+            if (tid == 0) s.n = (uint32_t)s.shared;
+            __syncthreads();
+            for (uint32_t i = tid; i < min(s.n, (uint32_t)CAP); i += PICK)
+                s.list[i] = __hip_atomic_load(&of_all[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
     }
     __syncthreads();
-    const bool list = s.n <= (uint32_t)CAP;
+    const bool list = s.n <= (uint32_t)CAP && !(by_bin && final > lists_to);
     const int listed = min((int)s.n, CAP);
     // Where no bin in question has more entries than a wave has lanes, its first wave goes on alone.
     const bool asked = tid == kb || tid == mb || (tid >= pb0 && tid <= pb1) || (tid >= sb0 && tid <= sb1);
-    const bool alone = list && listed <= 4096 && !__syncthreads_or(asked && count > FEW);
+    const bool alone = list && listed <= 512 && !__syncthreads_or(asked && count > FEW);
     if (alone && tid >= 64) return;
     auto sync = [&] {
         if (alone) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         else __syncthreads();
     };
-    auto pick = [&](auto counting, int b, uint64_t target) {
-        constexpr bool COUNT = decltype(counting)::value;
-        if (alone) return select_few<COUNT>(s, g, listed, b, target);
+    auto pick = [&](bool counting, int b, uint64_t target) {
+        if (alone) return select_few(s, counting, g, listed, b, target);
         const uint32_t n = s.count[b] - counted(b);
-        return list ? select_in<T, true, COUNT>(s, z, p.V, g, listed, b, n, target) : select_in<T, false, COUNT>(s, z, p.V, g, 0, b, n, target);
+        if (list) return n <= PICK ? select_one_each(s, counting, g, listed, b, target) : select_in<T, true>(s, counting, z, p.V, g, listed, b, n, target);
+        __syncthreads();
+        if (tid == 0) s.n = 0;
+        __syncthreads();
+        fetch(s, z, 0, p.V, 1, g.lowest(b), g.highest(b), 0.f, 0.f, 0.f, 0.f);
+        __syncthreads();
+        const uint32_t all_in = s.n;
+        return all_in <= (uint32_t)CAP ? select_in<T, true>(s, counting, z, p.V, g, (int)all_in, b, n, target)
+                                       : select_in<T, false>(s, counting, z, p.V, g, 0, b, n, target);
     };
 
     double total = all;
     if (kb < BINS) {
-        const Found f = pick(std::true_type(), kb, (uint64_t)p.top_k - counted(kb) - 1);
+        const Found f = pick(true, kb, (uint64_t)p.top_k - counted(kb) - 1);
         total = before(kb) + s.factor[kb] * (double)f.sum;
     }
     if (p.top_p < 1.f) {
         const double x = (double)p.top_p * total;
         const int b = min(max(reach(x, false), pb0), pb1);
         const double y = ceil((x - before(b)) / s.factor[b]) - 1.;  // a sum that reaches x passes the whole number below it
-        const Found f = pick(std::false_type(), b, (uint64_t)fmax(y, 0.));
+        const Found f = pick(false, b, (uint64_t)fmax(y, 0.));
         total = fmin(total, before(b) + s.factor[b] * (double)f.sum);
     }
     if (mb < BINS) {  // the last entry that is large enough
@@ -673,7 +786,7 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
     }
     const int b = min(max(token_bin(total), sb0), sb1);
     const double x = ((inside ? fmax(u, 0.) * total : total) - before(b)) / s.factor[b];
-    const Found f = pick(std::false_type(), b, (uint64_t)fmax(inside ? x : rint(x) - 1., 0.));
+    const Found f = pick(false, b, (uint64_t)fmax(inside ? x : rint(x) - 1., 0.));
     if (tid == 0) {
         p.tok[row] = (int32_t)~(uint32_t)f.rank;
         p.conf[row] = (float)((double)f.weight * s.factor[b] / total);
@@ -682,33 +795,53 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Workspace: the parts' bins, their lists, and what is said about them.
-struct Space {
-    size_t lists, abouts, total;
-    Space(int M, int V)
+// How a call is cut.  Parts are as short as leaves a row 20 of them (the second kernel adds them up) and the call 384 workgroups of parts twice as
+// long: 32 x 152064 take 31.8 us by parts of 8192, 32.7 by 16384 and 37.8 by 4096, one row of 32000 24.0 by 4096 and 27.1 by 8192, 400 x 9001 74.9 by
+// 16384 and 78.6 by 8192.  Where a row's lists do not do, its entries are fetched by as many workgroups as there are compute units to a row, of SLICE bytes
+// at least: the handing over takes 4 us (33 x 32001 fp32: 32.4 us with one, 36.7 with two), a workgroup reads 20 GB/s (32 x 152064 fp32: 70 us
+// with one, 58 with six).
+// The workspace has the parts' bins, their lists, what is said about them, and what the slices fetch.
+struct Plan {
+    int part, parts, slices;
+    size_t lists, abouts, shared, fetched, total;
+    Plan(int dtype, int M, int V)
     {
-        const size_t parts = (size_t)M * parts_of(V);
-        lists = align256(parts * BINS * sizeof(uint64_t));
-        abouts = lists + align256(parts * LIST * sizeof(uint64_t));
-        total = abouts + parts * sizeof(Part);
+        constexpr int CUS = 256, SLICE = 96 << 10;
+        const int size = dtype == FC_F32 ? 4 : 2;
+        auto parts_of = [&](int entries) { return (V + entries - 1) / entries; };
+        part = SHORT;
+        while (part < LONG && (parts_of(part) > 20 || (int64_t)M * parts_of(2 * part) >= 384)) part *= 2;
+        parts = parts_of(part);
+        slices = M >= CUS ? 1 : CUS / M;
+        const int most = (int)((int64_t)V * size / SLICE);
+        if (slices > most) slices = most > 1 ? most : 1;
+        const size_t n = (size_t)M * parts;
+        lists = align256(n * BINS * sizeof(uint64_t));
+        abouts = lists + align256(n * LIST * sizeof(uint64_t));
+        shared = abouts + align256(n * sizeof(Part));
+        fetched = shared + align256((size_t)M * sizeof(uint64_t));
+        total = fetched + (slices > 1 ? (size_t)M * CAP * sizeof(uint64_t) : 0);
     }
 };
 
 template <typename T>
 void launch(const FcSampleArgs &p, hipStream_t s)
 {
-    const int parts = parts_of(p.V);
-    const Space w(p.M, p.V);
+    const Plan w(sizeof(T) == 4 ? FC_F32 : FC_BF16, p.M, p.V);
     char *at = (char *)p.workspace;
-    uint64_t *bins = (uint64_t *)at, *lists = (uint64_t *)(at + w.lists);
+    uint64_t *bins = (uint64_t *)at, *lists = (uint64_t *)(at + w.lists), *fetched = (uint64_t *)(at + w.fetched);
     Part *abouts = (Part *)(at + w.abouts);
-    k_sample_bins<T><<<dim3((unsigned)(parts * p.M)), dim3(SCAN), 0, s>>>(p, parts, bins, lists, abouts);
-    k_sample_pick<T><<<dim3((unsigned)p.M), dim3(PICK), 0, s>>>(p, parts, bins, lists, abouts);
+    unsigned long long *shared = (unsigned long long *)(at + w.shared);
+    const dim3 grid((unsigned)(w.parts * p.M));
+    if (w.part == LONG) k_sample_bins<T, LONG><<<grid, dim3(SCAN), 0, s>>>(p, w.parts, bins, lists, abouts, shared);
+    else if (w.part == 2 * SHORT) k_sample_bins<T, 2 * SHORT><<<grid, dim3(SCAN), 0, s>>>(p, w.parts, bins, lists, abouts, shared);
+    else k_sample_bins<T, SHORT><<<grid, dim3(SCAN), 0, s>>>(p, w.parts, bins, lists, abouts, shared);
+    k_sample_pick<T><<<dim3((unsigned)p.M, (unsigned)w.slices), dim3(PICK), 0, s>>>(p, w.parts, bins, lists, abouts, shared, fetched);
 }
 
 }  // namespace
 
-size_t fc_sample_workspace(int dtype, int M, int V) { return Space(M, V).total; }
+size_t fc_sample_workspace(int dtype, int M, int V) { return Plan(dtype, M, V).total; }
 
 hipError_t fc_launch_sample(const FcSampleArgs &args, int dtype, hipStream_t s)
 {
