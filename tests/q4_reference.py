@@ -64,11 +64,12 @@ def attend(q, k, v, n, scale, pos=None):
 
 
 def attention_bound(ref, spread, score, most, n, dh, dtype):
-    """Largest error per element.  Scores: products of dh terms summed in fp32, dh + 4 roundings of 2^-24 of the sum of magnitudes (and, bf16, queries
-    held to 2^-22 of the row's largest in two 8-bit parts: within the same); the error of a score is the relative error of its weight,
-    in numerator and in sum.  Sums over n keys in fp32: n + 8 roundings.  bf16: weights rounded to fp16 (2^-11, or half a subnormal step, 2^-25 of at
-    most the largest), partial results of key ranges to fp16 of values normalised by their own sum (2^-11 of the largest |v|), the
-    output to bfloat16 (2^-8)."""
+    """Largest error per element.  Scores: products of dh terms summed in fp32, dh + 4 roundings of 2^-24 of the sum of magnitudes (fp32 queries are held to
+    2^-29 of the largest of 32 elements: within the same); the error of a score is the relative error of its weight, in numerator and in
+    sum.  Sums over n keys in fp32: n + 8 roundings; an fp32 weight is two fp16 numbers, 2^-23 of itself: within the same.  bf16: weights
+    rounded to fp16 (2^-11, or half a subnormal step, 2^-25 of at most the largest), queries in three 6-bit parts, which lack up to 2^-14 of the largest
+    of 32 elements, terms of either sign: 2^-11 of the largest |v| where keys of several tiles differ by it; the output to bfloat16
+    (2^-8)."""
     n = np.asarray(n).reshape(-1, 1, 1, 1)
     u = 2.0 ** -24
     err = (2 * (dh + 4) * u * score + (n + 8) * u) * spread
