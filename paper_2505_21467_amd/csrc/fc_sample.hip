@@ -50,7 +50,7 @@ constexpr Factors factors()
     }
     return f;
 }
-static_assert(BINS / PER_T == 32, "five powers");
+static_assert(BINS == 1024 && PER_T == 32, "five powers of 1/e; a wave searches 16 x 64 bins");
 __constant__ const Factors FACTORS = factors();
 
 // Order of the entries as a number: the larger logit first, then the smaller index.  -0 is 0.
@@ -122,12 +122,10 @@ struct Piece {
         else *this = __builtin_bit_cast(Piece, __builtin_bit_cast(unsigned __int128, *this) >> (back * BITS) | least << ((N - back) * BITS));
     }
     __device__ __forceinline__ float get(int j) const { return fc_to_float(v[j]); }
-    __device__ __forceinline__ float at(int j) const  // (any j: a shift, not an index)
+    __device__ __forceinline__ void next4()  // the upper half of eight
     {
-        struct halves { uint64_t v[2]; };
-        const halves h = __builtin_bit_cast(halves, *this);
-        const uint32_t x = (uint32_t)((j < N / 2 ? h.v[0] : h.v[1]) >> (j % (N / 2) * BITS));
-        return sizeof(T) == 2 ? __uint_as_float(x << 16) : __uint_as_float(x);
+#pragma unroll
+        for (int j = 0; j + 4 < N; ++j) v[j] = v[j + 4];
     }
     static constexpr uint64_t LEAST = sizeof(T) == 2 ? 0xff80ff80ff80ff80ull : 0xff800000ff800000ull;
 };
@@ -268,21 +266,36 @@ __global__ __launch_bounds__(SCAN) void k_sample_bins(FcSampleArgs p, int parts,
             const int first = from + s_piece[i] * N;
             Piece<T> x;
             x.load(z, first, to);
-            uint32_t in = 0;
-#pragma unroll
-            for (int j = 0; j < N; ++j) in |= x.get(j) >= cut ? 1u << j : 0;
+            // four entries at a time: their chains of fp64 operations overlap, and the wave takes places in the list for all at once
 #pragma unroll 1
-            while (in) {
-                const int j = __builtin_ctz(in);
-                in &= in - 1;
-                const float v = x.at(j);
-                double within;
-                const int bin = g.bin(v, within);
-                if (bin > last) continue;
-                atomicAdd(&s_bin[bin], (unsigned long long)(1ull << SUM_BITS | g.weight(within)));
-                if (bin > end) continue;
-                const uint32_t place = atomicAdd(&s_n, 1u);
-                if (place < LIST) list[at * LIST + place] = rank_of(v, (uint32_t)(first + j));
+            for (int j0 = 0; j0 < N; j0 += 4) {
+                int bin[4];
+                uint64_t w[4], listed[4];
+                uint32_t n = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    double within;
+                    bin[j] = g.bin(x.get(j), within);
+                    w[j] = g.weight(within);
+                    listed[j] = __ballot(bin[j] <= end);
+                    n += (uint32_t)__builtin_popcountll(listed[j]);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (bin[j] <= last) atomicAdd(&s_bin[bin[j]], (unsigned long long)(1ull << SUM_BITS | w[j]));
+                if (n) {
+                    const int leader = __builtin_ctzll(__ballot(true));
+                    uint32_t place = 0;
+                    if (tid % 64 == leader) place = atomicAdd(&s_n, n);
+                    place = (uint32_t)__builtin_amdgcn_readlane((int)place, leader);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t own = __builtin_amdgcn_mbcnt_hi((uint32_t)(listed[j] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)listed[j], place));
+                        if (bin[j] <= end && own < LIST) list[at * LIST + own] = rank_of(x.get(j), (uint32_t)(first + j0 + j));
+                        place += (uint32_t)__builtin_popcountll(listed[j]);
+                    }
+                }
+                x.next4();
             }
         }
     }
@@ -628,14 +641,16 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
 
     auto before = [&](int b) { return b > 0 ? s.cum[b - 1] : 0.; };
     auto counted = [&](int b) { return b > 0 ? s.count[b - 1] : 0u; };
-    // The first bin whose running sum reaches x, or (past) exceeds it; BINS if none does.
-    auto reach = [&](double x, bool past) {
-        int b = 0;
-#pragma unroll 1
-        for (int step = BINS / 2; step; step >>= 1)
-            if (past ? s.cum[b + step - 1] <= x : s.cum[b + step - 1] < x) b += step;
-        return (past ? s.cum[b] <= x : s.cum[b] < x) ? BINS : b;
+    // The first bin at whose end `enough` holds (it does from there on), BINS if at none: the wave's lanes look at every sixteenth, then at sixteen.
+    auto search = [&](auto enough) {
+        const int lane = tid % 64;
+        const uint64_t sixteen = __ballot(enough(lane * 16 + 15));
+        if (!sixteen) return BINS;
+        const int b = __builtin_ctzll(sixteen) * 16;
+        return b + __builtin_ctzll(__ballot(enough(b + lane % 16)));
     };
+    // ... whose running sum reaches x, or (past) exceeds it.
+    auto reach = [&](double x, bool past) { return search([&](int b) { return past ? s.cum[b] > x : s.cum[b] >= x; }); };
     const double all = s.cum[BINS - 1], u = p.greedy ? 0. : (double)p.u[row];
     const bool inside = u < 1.;  // (NaN: not)
     // The bin of the token for this total of kept weights: where u times it is exceeded, or the last kept entry's.
@@ -648,10 +663,7 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
     double low = all, high = all;
     int kb = BINS, mb = BINS, pb0 = BINS, pb1 = -1;
     if (p.top_k > 0 && s.count[BINS - 1] >= (uint32_t)p.top_k) {  // (otherwise what is kept beyond the bins weighs nothing)
-        kb = 0;
-#pragma unroll 1
-        for (int step = BINS / 2; step; step >>= 1)
-            if (s.count[kb + step - 1] < (uint32_t)p.top_k) kb += step;
+        kb = search([&](int b) { return s.count[b] >= (uint32_t)p.top_k; });
         low = before(kb);
         high = s.cum[kb];
     }
