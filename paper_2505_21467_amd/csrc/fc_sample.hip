@@ -171,11 +171,13 @@ __device__ __forceinline__ X wave_scan(X x)
     return wave_run(x, [](X a, X b) { return a + b; });
 }
 
-// What is kept of a part besides its bins: the largest logit; the last bin of which the list has every entry (-1: none); their number.
-struct Part {
+// What is kept of a part besides its bins: the largest logit; the last bin of which the list has every entry (-1: none); their number; the last bin
+// that is kept (-1: none).
+struct __align__(16) Part {
     float largest;
     int32_t bin;
     uint32_t n;
+    int32_t last;
 };
 
 // One part of a row: bins[] gets (entries << 48 | sum of weights), list[] the ranks of some 256 of its largest entries.
@@ -224,7 +226,7 @@ __global__ __launch_bounds__(SCAN) void k_sample_bins(FcSampleArgs p, int parts,
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < SCAN / 64; ++i) top = fmaxf(top, s_max[i]);
-    int end = -1;
+    int end = -1, last = -1;
     if (top > -__builtin_inff()) {
         const Grid g(top, p.inv_t * PER_T);
         // (in fp32: at most two bins above the exact one)
@@ -245,7 +247,7 @@ __global__ __launch_bounds__(SCAN) void k_sample_bins(FcSampleArgs p, int parts,
         for (int i = 0; i < 2; ++i)
             if (run >= ks[i] && run - a - b < ks[i]) s_last[i] = run - b >= ks[i] ? 2 * tid : 2 * tid + 1;
         __syncthreads();
-        const int last = min(min(p.last_bin, BINS - 1), s_last[0] + 2);
+        last = min(min(p.last_bin, BINS - 1), s_last[0] + 2);
         end = min(last, s_last[1] + 2);
         const float cut = g.lowest(last);
         // Pieces with an entry that matters are listed, spread over the threads and read again: under a top-k of 50 one entry in hundreds does, and every
@@ -300,9 +302,9 @@ __global__ __launch_bounds__(SCAN) void k_sample_bins(FcSampleArgs p, int parts,
         }
     }
     __syncthreads();
-    for (int i = tid; i < BINS; i += SCAN) bins[at * BINS + i] = s_bin[i];
+    for (int i = tid; i <= last; i += SCAN) bins[at * BINS + i] = s_bin[i];
     if (tid == 0 && part == 0) shared[row] = 0;
-    if (tid == 0) about[at] = Part{top, s_n <= LIST ? end : -1, min(s_n, (uint32_t)LIST)};
+    if (tid == 0) about[at] = Part{top, s_n <= LIST ? end : -1, min(s_n, (uint32_t)LIST), last};
 }
 
 struct Entry {
@@ -605,17 +607,18 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
 #pragma unroll 1
         for (int i = 0; i < m; i += 8) {
             uint64_t x[8];
-            int at[8];
+            int at[8], last[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 const int from = min(i + k, m - 1);
                 at[k] = i + k < m ? tid - __builtin_amdgcn_readlane(off, from) : -1;
-                x[k] = part[(size_t)(i0 + from) * BINS + max(at[k], 0)];
+                last[k] = __builtin_amdgcn_readlane(a.last, from);
+                x[k] = part[(size_t)(i0 + from) * BINS + max(min(at[k], last[k]), 0)];
             }
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                count += at[k] >= 0 ? (uint32_t)(x[k] >> SUM_BITS) : 0;
-                sum += at[k] >= 0 ? x[k] & ((1ull << SUM_BITS) - 1) : 0;
+                count += at[k] >= 0 && at[k] <= last[k] ? (uint32_t)(x[k] >> SUM_BITS) : 0;
+                sum += at[k] >= 0 && at[k] <= last[k] ? x[k] & ((1ull << SUM_BITS) - 1) : 0;
             }
         }
     }
