@@ -20,10 +20,15 @@ struct Q4Place {
 template <typename T>
 struct Eight {
     uint4 raw[sizeof(T) / 2];
+    template <bool ONCE>  // with the non-temporal hint
     __device__ __forceinline__ void load(const T *p)
     {
+        typedef uint32_t any __attribute__((ext_vector_type(4), aligned(2)));
 #pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) raw[i] = fc_load_any<uint4>(p + i * 16 / sizeof(T));
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+            const T *at = p + i * 16 / sizeof(T);
+            raw[i] = ONCE ? __builtin_bit_cast(uint4, __builtin_nontemporal_load((const any *)at)) : fc_load_any<uint4>(at);
+        }
     }
     __device__ __forceinline__ void get(float (&x)[8]) const
     {
@@ -133,9 +138,11 @@ __device__ __forceinline__ uint32_t q4_spread(uint32_t x)
 // thread takes the eight rows of a word of the tile, so that nothing is turned.
 //
 // Bound by memory where there is much to store; a block is one latency chain.  All that a thread loads is in flight at once, 16 bytes a lane next to
-// one another on both sides: 4 x 32 heads x 4096 rows (268 MB in, 71 MB out) take 61 us, 5.5 TB/s, and as long to read back, where a large copy
-// reaches 4.9; with a block of 32 elements a thread and a byte per value code in LDS both took 107 us.  19 entries: 5 us.
-template <typename T, int DH, bool FROM_CACHE>
+// one another on both sides.  4 x 32 heads x 4096 rows from HBM (268 MB in, 71 MB out) take 54 us with the non-temporal hint (ONCE: rows that exceed the
+// memory-side cache) and 80 .. 88 without; reading them back 56 .. 64, 5.4 TB/s and more, where a large copy reaches 4.9.  4 x 8192 rows in
+// fp32 that are in that cache: 8.7 us without the hint, 10.1 with it.  A block of 32 elements a thread and a byte per value code in LDS took
+// 107 us each way.  19 entries: 5 us.
+template <typename T, int DH, bool FROM_CACHE, bool ONCE>
 __global__ __launch_bounds__(2 * DH) void k_q4_store(uint8_t *layer, const T *__restrict__ k, const T *__restrict__ v, Q4Place p, int max_seq,
                                                   int tiles, int rows_or_spad, int Hkv)
 {
@@ -194,8 +201,8 @@ __global__ __launch_bounds__(2 * DH) void k_q4_store(uint8_t *layer, const T *__
         // (rows that are not stored: another one's elements)
         const int src = FROM_CACHE ? tile * FC_VTILE + r : p.pos ? max(s_src[r], 0) : min(max(tile * FC_VTILE + r - p.start, 0), p.rows - 1);
         const size_t at = (pair * (size_t)rows_or_spad + src) * DH + lane * 8;
-        kx[i].load(k + at);
-        if (!FROM_CACHE) vx[i].load(v + at);
+        kx[i].template load<ONCE>(k + at);
+        if (!FROM_CACHE) vx[i].template load<ONCE>(v + at);
     }
     struct __align__(4 * sizeof(T)) Four { T v[4]; };  // (the cache's values: aligned)
     Four four[PASSES][2];
@@ -365,9 +372,11 @@ void launch_store(const FcQ4Geom &G, uint8_t *layer, const void *k, const void *
     const dim3 grid((unsigned)n, (unsigned)(G.B * G.Hkv));
     const Q4Place p{pos, start, rows, rows < tiles};
     if (src_spad)
-        k_q4_store<T, DH, true><<<grid, dim3(2 * DH), 0, s>>>(layer, (const T *)k, (const T *)v, p, G.max_seq, tiles, src_spad, G.Hkv);
+        k_q4_store<T, DH, true, false><<<grid, dim3(2 * DH), 0, s>>>(layer, (const T *)k, (const T *)v, p, G.max_seq, tiles, src_spad, G.Hkv);
+    else if (fc_read_once((double)G.B * G.Hkv * rows * (2.0 * DH * sizeof(T) + fc_q4_tile_bytes(DH) / 64)))  // (in and out)
+        k_q4_store<T, DH, false, true><<<grid, dim3(2 * DH), 0, s>>>(layer, (const T *)k, (const T *)v, p, G.max_seq, tiles, rows, G.Hkv);
     else
-        k_q4_store<T, DH, false><<<grid, dim3(2 * DH), 0, s>>>(layer, (const T *)k, (const T *)v, p, G.max_seq, tiles, rows, G.Hkv);
+        k_q4_store<T, DH, false, false><<<grid, dim3(2 * DH), 0, s>>>(layer, (const T *)k, (const T *)v, p, G.max_seq, tiles, rows, G.Hkv);
 }
 
 template <typename T, int DH>

@@ -297,3 +297,23 @@ def test_tensors_at_any_element():
     fc.fc_q4_attention(c.handle, 0, at(q), 5, 93, None, None, o[1:], ws)
     plain = c.attend(q, 93)
     assert np.array_equal(ref.f64(o[1:-1]).reshape(plain.shape), plain) and o[0] == 3 and o[-1] == 3
+
+
+@pytest.mark.parametrize("dtype,Dh,B,rows", [("bf16", 128, 4, 4200), ("f32", 64, 4, 4333)])
+def test_rows_beyond_what_a_cache_holds(dtype, Dh, B, rows):
+    """More than 256 MB of rows in one call, which take another kind of load."""
+    Hkv = 32 if dtype == "bf16" else 34
+    c = Cache(dtype, B, Hkv, Hkv, Dh, rows + 9)
+    g = torch.Generator(DEV).manual_seed(24)
+    k, v = (torch.randn((B, Hkv, rows, Dh), generator=g, device=DEV).to(c.tdt) for _ in "kv")
+    c.store(k, v, start=5)
+    gk, gv = (torch.empty((B, Hkv, rows + 9, Dh), dtype=c.tdt, device=DEV) for _ in "kv")
+    fc.fc_q4_read_rows(c.handle, 0, gk, gv, 0, rows + 9)
+    for b, h in ((0, 0), (1, Hkv // 2), (B - 1, Hkv - 1)):
+        hk, hv = ref.held_rows(ref.f64(k[b, h]), ref.f64(v[b, h]))
+        assert np.array_equal(ref.f64(gk[b, h, 5:5 + rows]), hk) and np.array_equal(ref.f64(gv[b, h, 5:5 + rows]), hv)
+    small = Cache(dtype, B, Hkv, Hkv, Dh, rows + 9)           # the same rows in two calls: the other kind
+    half = rows // 2
+    for a, b in ((0, half), (half, rows)):
+        small.store(k[:, :, a:b].contiguous(), v[:, :, a:b].contiguous(), start=5 + a)
+    assert torch.equal(c.storage, small.storage)
