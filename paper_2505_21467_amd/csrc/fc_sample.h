@@ -11,7 +11,8 @@ struct FcSampleArgs {
     float top_p, min_p;
     double inv_t;  // 1 / temperature (1 where that is 0)
     int32_t greedy;
-    double log_min_p;  // set by the launch, as is the next
+    double log_min_p;  // set by the launch, as are the next two
+    double bin_width;  // in units of a logit
     int32_t last_bin;  // the last bin that can matter
     const float *u;
     int32_t *tok;

@@ -69,8 +69,8 @@ __device__ __forceinline__ float logit_of(uint64_t rank)
 struct Grid {
     float most;
     bool infinite;  // then the infinite logits are in bin 0, and no others in any
-    double c, top;  // bins to a unit of logit; the largest logit's bin
-    __device__ __forceinline__ Grid(float most_, double c_) : most(most_), infinite(most_ > 3.4028235e38f), c(c_), top(floor((double)most_ * c_)) {}
+    double c, by_c, top;  // bins to a unit of logit, 1 / that; the largest logit's bin
+    __device__ __forceinline__ Grid(float most_, double c_, double by_c_) : most(most_), infinite(most_ > 3.4028235e38f), c(c_), by_c(by_c_), top(floor((double)most_ * c_)) {}
     __device__ __forceinline__ int bin(float z, double &within) const
     {
 #pragma clang fp contract(off)  // (x is rounded: with one fused operation for x - b an entry's weight would depend on where it is computed)
@@ -91,12 +91,12 @@ struct Grid {
     // Logits of bins b0 .. b1, and perhaps a few more on either side.
     __device__ __forceinline__ float lowest(int b1) const
     {
-        const float x = (float)((top - b1) / c);
+        const float x = (float)((top - b1) * by_c);
         return infinite ? most : x - fabsf(x) * 3e-7f;
     }
     __device__ __forceinline__ float highest(int b0) const
     {
-        const float x = (float)((top - b0 + 1.) / c);
+        const float x = (float)((top - b0 + 1.) * by_c);
         return infinite ? most : x + fabsf(x) * 3e-7f;
     }
 };
@@ -171,6 +171,18 @@ __device__ __forceinline__ X wave_scan(X x)
     return wave_run(x, [](X a, X b) { return a + b; });
 }
 
+// Sum over the waves before this one, of what every wave's last lane has left in LDS.  (Reads one by one cost 0.3 us more.)
+template <int WAVES, typename X>
+__device__ __forceinline__ X sum_before(const X *of_wave)
+{
+    const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    struct words { int v[sizeof(X) / 4]; };
+    words w = __builtin_bit_cast(words, wave_scan(lane < wave ? of_wave[lane % WAVES] : X(0)));
+#pragma unroll
+    for (int &v : w.v) v = __builtin_amdgcn_readlane(v, 63);
+    return __builtin_bit_cast(X, w);
+}
+
 // What is kept of a part besides its bins: the largest logit; the last bin of which the list has every entry (-1: none); their number; the last bin
 // that is kept (-1: none).
 struct __align__(16) Part {
@@ -228,7 +240,7 @@ __global__ __launch_bounds__(SCAN) void k_sample_bins(FcSampleArgs p, int parts,
     for (int i = 0; i < SCAN / 64; ++i) top = fmaxf(top, s_max[i]);
     int end = -1, last = -1;
     if (top > -__builtin_inff()) {
-        const Grid g(top, p.inv_t * PER_T);
+        const Grid g(top, p.inv_t * PER_T, p.bin_width);
         // (in fp32: at most two bins above the exact one)
         const float c = (float)g.c;
 #pragma unroll
@@ -241,7 +253,7 @@ __global__ __launch_bounds__(SCAN) void k_sample_bins(FcSampleArgs p, int parts,
         uint32_t run = wave_scan(a + b);
         if (tid % 64 == 63) s_wave[tid / 64] = run;
         __syncthreads();
-        for (int i = 0; i < tid / 64; ++i) run += s_wave[i];
+        run += sum_before<SCAN / 64>(s_wave);
         const uint32_t ks[2] = {p.top_k > 0 ? (uint32_t)p.top_k : 0xffffffffu, (uint32_t)min(max(p.top_k, LISTED), 2 * LISTED)};
 #pragma unroll
         for (int i = 0; i < 2; ++i)
@@ -311,6 +323,14 @@ struct Entry {
     uint64_t rank, weight;
 };
 
+// Where a row's targets can lie: the bins in which top-k, min-p and top-p end (BINS: none, -1 the end of none) and in which the token is; the last of
+// them all; the logits to fetch; whether those are too many for the list; whether no bin in question has more entries than a wave has lanes.
+struct Aim {
+    int kb, mb, pb0, pb1, sb0, sb1, final, ranges;
+    float least[3], most[3];
+    bool by_bin, few;
+};
+
 struct PickShared {
     double cum[BINS];       // running sums of weights over the bins, from the largest logit down, in units of 2^-32 of bin 0's upper edge
     double factor[BINS];    // exp(-bin / 32)
@@ -323,6 +343,7 @@ struct PickShared {
     uint64_t digit_sum[256];
     uint32_t digit_count[256];
     Entry few[FEW];
+    Aim aim;
     unsigned long long ones, zeros, shared, sum_found, rank_found, weight_found;
     uint32_t n, digit, count_found;
 };
@@ -589,7 +610,7 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
         }
         return;
     }
-    const Grid g(z_max, p.inv_t * PER_T);
+    const Grid g(z_max, p.inv_t * PER_T, p.bin_width);
 
     // Thread i: bin i of the row, eight parts in flight together.  (lists_to: the last bin of which the parts' lists have every entry.)
     uint32_t count = 0;
@@ -634,10 +655,8 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
     s.factor[tid] = factor;
     if (tid == 0) s.n = 0;
     __syncthreads();
-    for (int i = 0; i < tid / 64; ++i) {
-        cum += s.wave_sum[i];
-        counts += s.wave_count[i];
-    }
+    cum += sum_before<PICK / 64>(s.wave_sum);
+    counts += sum_before<PICK / 64>(s.wave_count);
     s.cum[tid] = cum;
     s.count[tid] = counts;
     __syncthreads();
@@ -662,42 +681,60 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
         return b < BINS ? b : reach(all, false);
     };
 
-    // Where the targets can lie: the total is known but for the bins in which filters end.
-    double low = all, high = all;
-    int kb = BINS, mb = BINS, pb0 = BINS, pb1 = -1;
-    if (p.top_k > 0 && s.count[BINS - 1] >= (uint32_t)p.top_k) {  // (otherwise what is kept beyond the bins weighs nothing)
-        kb = search([&](int b) { return s.count[b] >= (uint32_t)p.top_k; });
-        low = before(kb);
-        high = s.cum[kb];
-    }
-    if (p.top_p < 1.f) {
-        pb0 = min(reach((double)p.top_p * low, false), BINS - 1);
-        pb1 = kb < BINS ? min(reach((double)p.top_p * high, false), BINS - 1) : pb0;
-        low = fmin(low, before(pb0));
-        high = fmin(high, s.cum[pb1]);
-    }
-    if (p.min_p > 0.f && !g.infinite) {
-        const double d = g.top - floor((double)z_max * g.c + p.log_min_p * PER_T);
-        if (d <= (double)min(kb, BINS - 1)) {  // (beyond the bin in which top-k ends it keeps more)
-            mb = (int)d;
-            low = fmin(low, before(mb));
-            high = fmin(high, s.cum[mb]);
+    // Where the targets can lie: the total is known but for the bins in which filters end.  One wave finds out, while the others leave it the compute
+    // unit.
+    if (tid < 64) {
+        double low = all, high = all;
+        int kb = BINS, mb = BINS, pb0 = BINS, pb1 = -1;
+        if (p.top_k > 0 && s.count[BINS - 1] >= (uint32_t)p.top_k) {  // (otherwise what is kept beyond the bins weighs nothing)
+            kb = search([&](int b) { return s.count[b] >= (uint32_t)p.top_k; });
+            low = before(kb);
+            high = s.cum[kb];
+        }
+        if (p.top_p < 1.f) {
+            pb0 = min(reach((double)p.top_p * low, false), BINS - 1);
+            pb1 = kb < BINS ? min(reach((double)p.top_p * high, false), BINS - 1) : pb0;
+            low = fmin(low, before(pb0));
+            high = fmin(high, s.cum[pb1]);
+        }
+        if (p.min_p > 0.f && !g.infinite) {
+            const double d = g.top - floor((double)z_max * g.c + p.log_min_p * PER_T);
+            if (d <= (double)min(kb, BINS - 1)) {  // (beyond the bin in which top-k ends it keeps more)
+                mb = (int)d;
+                low = fmin(low, before(mb));
+                high = fmin(high, s.cum[mb]);
+            }
+        }
+        const int sb0 = token_bin(low), sb1 = low < high ? token_bin(high) : sb0;
+        // Logits of the bin in which top-k ends, of those in which the other filters can, and of the token's.  Where they lie apart with many entries
+        // between them, three ranges; else one.
+        const int f0 = min(pb0, mb), f1 = max(mb < BINS ? mb : -1, pb1), first = min(min(f0, kb), sb0), final = max(max(f1, kb < BINS ? kb : -1), sb1);
+        const bool apart = s.count[final] - counted(first) > CAP / 2;
+        auto entries = [&](int b0, int b1) { return b0 <= b1 && b1 < BINS ? s.count[b1] - counted(b0) : 0u; };
+        if (tid == 0) {
+            Aim a{kb, mb, pb0, pb1, sb0, sb1, final, apart ? 3 : 1, {}, {}, false, false};
+            a.least[0] = g.lowest(apart ? sb1 : final);
+            a.most[0] = g.highest(apart ? sb0 : first);
+            a.least[1] = f1 >= 0 ? g.lowest(f1) : __builtin_inff();
+            a.most[1] = f1 >= 0 ? g.highest(f0) : -__builtin_inff();
+            a.least[2] = kb < BINS ? g.lowest(kb) : __builtin_inff();
+            a.most[2] = kb < BINS ? g.highest(kb) : -__builtin_inff();
+            // (too many for the list: bin by bin, then)
+            a.by_bin = (apart ? entries(sb0, sb1) + entries(f0, f1) + entries(kb, kb) : entries(first, final)) > (uint32_t)CAP;
+            a.few = max(max(entries(kb, kb), entries(mb, mb)), max(entries(pb0, pb1), entries(sb0, sb1))) <= (uint32_t)FEW;
+            s.aim = a;
         }
     }
-    const int sb0 = token_bin(low), sb1 = low < high ? token_bin(high) : sb0;
-    // Logits of the bin in which top-k ends, of those in which the other filters can, and of the token's.  Where they lie apart with many entries between
-    // them, three ranges; else one.
-    const int f0 = min(pb0, mb), f1 = max(mb < BINS ? mb : -1, pb1), first = min(min(f0, kb), sb0), final = max(max(f1, kb < BINS ? kb : -1), sb1);
-    const bool apart = s.count[final] - counted(first) > CAP / 2;
-    const float none = __builtin_inff();
-    const float slow = g.lowest(apart ? sb1 : final), shigh = g.highest(apart ? sb0 : first);
-    const float flow = apart && f1 >= 0 ? g.lowest(f1) : none, fhigh = apart && f1 >= 0 ? g.highest(f0) : -none;
-    const float klow = apart && kb < BINS ? g.lowest(kb) : none, khigh = apart && kb < BINS ? g.highest(kb) : -none;
-    auto wanted = [&](float x) { return (x >= slow && x <= shigh) || (apart && ((x >= flow && x <= fhigh) || (x >= klow && x <= khigh))); };
-    auto within = [&](int b0, int b1) { return b0 <= b1 && b1 < BINS ? s.count[b1] - counted(b0) : 0u; };
-    // (too many for the list: bin by bin, then)
-    const bool by_bin = (apart ? within(sb0, sb1) + within(f0, f1) + within(kb, kb) : within(first, final)) > (uint32_t)CAP;
-    if (final <= lists_to) {  // a wave to a part
+    __syncthreads();
+    const Aim aim = s.aim;
+    const int kb = aim.kb, mb = aim.mb, pb0 = aim.pb0, pb1 = aim.pb1, sb0 = aim.sb0, sb1 = aim.sb1;
+    const bool listed_all = aim.final <= lists_to, by_bin = aim.by_bin && !listed_all;
+    auto wanted = [&](float x) {
+        bool in = x >= aim.least[0] && x <= aim.most[0];
+        if (aim.ranges > 1) in |= (x >= aim.least[1] && x <= aim.most[1]) || (x >= aim.least[2] && x <= aim.most[2]);
+        return in;
+    };
+    if (listed_all) {  // a wave to a part
         if (slice) return;
 #pragma unroll 1
         for (int i = tid / 64; i < parts; i += PICK / 64) {
@@ -719,7 +756,7 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
         if (slice) return;
     } else {
         const int per = ((p.V + slices - 1) / slices + 7) / 8 * 8;
-        fetch(s, z, slice * per, min(p.V, (slice + 1) * per), apart ? 3 : 1, slow, shigh, flow, fhigh, klow, khigh);
+        fetch(s, z, slice * per, min(p.V, (slice + 1) * per), aim.ranges, aim.least[0], aim.most[0], aim.least[1], aim.most[1], aim.least[2], aim.most[2]);
         if (slices > 1) {  // the last one to come finds what all have fetched
             __syncthreads();
             const uint32_t own = s.n;
@@ -743,11 +780,10 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
         }
     }
     __syncthreads();
-    const bool list = s.n <= (uint32_t)CAP && !(by_bin && final > lists_to);
+    const bool list = s.n <= (uint32_t)CAP && !by_bin;
     const int listed = min((int)s.n, CAP);
     // Where no bin in question has more entries than a wave has lanes, its first wave goes on alone.
-    const bool asked = tid == kb || tid == mb || (tid >= pb0 && tid <= pb1) || (tid >= sb0 && tid <= sb1);
-    const bool alone = list && listed <= 512 && !__syncthreads_or(asked && count > FEW);
+    const bool alone = list && listed <= 512 && aim.few;
     if (alone && tid >= 64) return;
     auto sync = [&] {
         if (alone) __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -862,6 +898,7 @@ hipError_t fc_launch_sample(const FcSampleArgs &args, int dtype, hipStream_t s)
 {
     FcSampleArgs p = args;
     p.log_min_p = p.min_p > 0.f ? log((double)p.min_p) : 0.;
+    p.bin_width = 1. / (p.inv_t * PER_T);
     // With nothing but min-p to sum up to, entries below it need not be counted (two bins for the roundings).
     p.last_bin = BINS - 1;
     if (p.min_p > 0.f && !(p.top_p < 1.f) && -p.log_min_p * PER_T < BINS - 3) p.last_bin = (int)(-p.log_min_p * PER_T) + 2;
