@@ -848,9 +848,9 @@ size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // How a call is cut.  Parts are as short as leaves a row 20 of them (the second kernel adds them up) and the call 384 workgroups of parts twice as
 // long: 32 x 152064 take 31.8 us by parts of 8192, 32.7 by 16384 and 37.8 by 4096, one row of 32000 24.0 by 4096 and 27.1 by 8192, 400 x 9001 74.9 by
-// 16384 and 78.6 by 8192.  Where a row's lists do not do, its entries are fetched by as many workgroups as there are compute units to a row, of SLICE bytes
-// at least: the handing over takes 4 us (33 x 32001 fp32: 32.4 us with one, 36.7 with two), a workgroup reads 20 GB/s (32 x 152064 fp32: 70 us
-// with one, 58 with six).
+// 16384 and 78.6 by 8192.  Where a row's lists do not do, rows of 256 KB and more are fetched by as many workgroups as there are compute units to a
+// row, of SLICE bytes at least: the handing over takes 4 us (57 rows of 50001 fp32: 32.4 us with one workgroup, 36.7 with two), and a workgroup
+// reads 20 GB/s (32 x 152064 fp32: 70 us with one, 58 with six; 8 x 152064 bf16 42.6 with one, 37.2 with three).
 // The workspace has the parts' bins, their lists, what is said about them, and what the slices fetch.
 struct Plan {
     int part, parts, slices;
@@ -864,8 +864,9 @@ struct Plan {
         while (part < LONG && (parts_of(part) > 20 || (int64_t)M * parts_of(2 * part) >= 384)) part *= 2;
         parts = parts_of(part);
         slices = M >= CUS ? 1 : CUS / M;
-        const int most = (int)((int64_t)V * size / SLICE);
-        if (slices > most) slices = most > 1 ? most : 1;
+        const int64_t row = (int64_t)V * size;
+        const int most = row < 256 << 10 ? 1 : (int)(row / SLICE);
+        if (slices > most) slices = most;
         const size_t n = (size_t)M * parts;
         lists = align256(n * BINS * sizeof(uint64_t));
         abouts = lists + align256(n * LIST * sizeof(uint64_t));
