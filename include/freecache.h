@@ -82,7 +82,7 @@ const char *fc_last_error(void);
  * workgroup), FC_ATTN_WGS, FC_LIN_WGS, FC_ACCEPT_WGS (target workgroup counts), FC_LIN_NO_ROWS,
  * FC_GEMM_NO_SPLIT, FC_PROJ_NO_HEADSPLIT (any value switches the named path off), FC_LIN_WIDE_SHAPE,
  * FC_PROJ_GEMM_SHAPE (0..11: one GEMM tile shape for everything), FC_LIN_KSPLIT (parts of the hidden
- * dimension).  Host only; not thread-safe against concurrent calls into the library; workspace sizes
+ * dimension), FC_Q4_TILES ("R,W,S": row tiles, waves and key ranges of fc_q4_attention).  Host only; not thread-safe against concurrent calls into the library; workspace sizes
  * depend on the knobs, so query them after setting.
  * Errors: INVALID_ARG (NULL or unknown name). */
 fc_status fc_tuning_set(const char *name, const char *value);
@@ -422,7 +422,8 @@ fc_status fc_gather_rows(int32_t dtype, const void *table, int32_t rows, int32_t
  * temperature 0 is the arg-max with conf = softmax(z)[tok] as in fc_lm_head_argmax; top_k, top_p, min_p and u are then not looked at.
  * A row gives the same bits from call to call and whatever else is in the batch.  Weights are exact to 2^-33 of themselves; entries 32 temperatures and more
  * below the largest (w < 1.3e-14) count as w = 0.  NaN entries are passed over, -inf ones have w = 0; of several +inf each has w = 1 and
- * the finite ones 0.  A row of nothing but NaN and -inf gets tok = -1, conf = 0.
+ * the finite ones 0.  A row of nothing but NaN and -inf gets tok = -1, conf = 0 (fc_unmask_select would write that -1: it is the caller's to
+ * look for).
  */
 
 /* Workspace bytes of fc_sample_tokens for this shape; 0 on bad arguments. */
