@@ -280,7 +280,8 @@ size_t fc_q4_workspace_bytes(const fc_config *cfg, int32_t max_rows);
  *   out      device [B][A][Hq*Dh]
  *   workspace  device, 16-byte aligned, may be NULL.  Two calls that overlap in time must not share one.
  * Rows behind a sequence's length are not looked at: whatever they hold does not matter.
- * Errors: INVALID_ARG, BOUNDS (layer; kv_len < 1 or > max_seq), UNSUPPORTED (batch * A beyond 2^24), HIP. */
+ * Errors: INVALID_ARG, BOUNDS (layer; kv_len < 1 or > max_seq), UNSUPPORTED (batch * A beyond 2^24; beyond 2^23 row tiles: (batch * n_kv_heads +
+ * 7) times the 16-row tiles of A rows of a kv head's query heads), HIP. */
 fc_status fc_q4_attention(const fc_q4_cache *cache, int32_t layer, const void *q, int32_t A, int32_t kv_len, const int32_t *kv_lens,
                           const int32_t *pos, void *out, void *workspace, size_t workspace_bytes, void *stream);
 
@@ -433,7 +434,7 @@ size_t fc_sample_workspace_bytes(int32_t dtype, int32_t M, int32_t V);
  *   u       device float [M], uniform in [0, 1); below 0 counts as 0, 1 or more (and NaN) picks the last kept entry.  May be NULL at temperature 0.
  *   tok  device int32 [M];  conf  device float [M];  workspace  device, 16-byte aligned, >= fc_sample_workspace_bytes(dtype, M, V) bytes
  * Errors: INVALID_ARG (NULL; M, V < 1; ld < V; temperature < 0 or not finite; top_k < 0; top_p outside (0, 1]; min_p outside [0, 1]),
- * UNSUPPORTED (V beyond 2^24, M beyond 65535), WORKSPACE, HIP. */
+ * UNSUPPORTED (V beyond 2^24, M beyond 65535, M * V beyond 2^36), WORKSPACE, HIP.  Two calls that overlap in time must not share a workspace. */
 fc_status fc_sample_tokens(int32_t dtype, const void *logits, int64_t ld, int32_t M, int32_t V, float temperature, int32_t top_k,
                            float top_p, float min_p, const float *u, int32_t *tok, float *conf, void *workspace,
                            size_t workspace_bytes, void *stream);

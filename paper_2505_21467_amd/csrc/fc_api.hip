@@ -1486,7 +1486,8 @@ fc_status fc_q4_alloc(const fc_config *cfg, void *storage, fc_q4_cache **out)
     if (!storage) {
         const size_t bytes = fc_q4_storage_bytes(cfg);
         void *p = nullptr;
-        if (hipMalloc(&p, bytes) != hipSuccess || hipMemset(p, 0, bytes) != hipSuccess) {
+        // (and wait: the caller's stream need not be one that waits for the null stream)
+        if (hipMalloc(&p, bytes) != hipSuccess || hipMemset(p, 0, bytes) != hipSuccess || hipStreamSynchronize(nullptr) != hipSuccess) {
             (void)hipGetLastError();
             if (p) (void)hipFree(p);
             delete c;
@@ -1559,7 +1560,11 @@ fc_status fc_q4_attention(const fc_q4_cache *cache, int32_t layer, const void *q
     if (st != FC_OK) return st;
     if (!q || !out) return fail(FC_ERR_INVALID_ARG, "q or out is NULL");
     if (A < 1) return fail(FC_ERR_INVALID_ARG, "A %d must be >= 1", A);
-    if ((int64_t)A * cache->cfg.batch > (1 << 24)) return fail(FC_ERR_UNSUPPORTED, "batch * A exceeds 2^24 rows");
+    const fc_config &c = cache->cfg;
+    if ((int64_t)A * c.batch > (1 << 24)) return fail(FC_ERR_UNSUPPORTED, "batch * A exceeds 2^24 rows");
+    // (workgroups of up to 512 threads, of which a grid holds 2^32)
+    if (((int64_t)c.batch * c.n_kv_heads + 7) * (((int64_t)A * (c.n_q_heads / c.n_kv_heads) + 15) / 16) > (1 << 23))
+        return fail(FC_ERR_UNSUPPORTED, "more than 2^23 row tiles of 16 rows");
     if (kv_len < 1 || kv_len > cache->cfg.max_seq)
         return fail(FC_ERR_BOUNDS, "kv_len %d outside [1, %d]", kv_len, cache->cfg.max_seq);
     if ((uintptr_t)workspace & 15) return fail(FC_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
@@ -1595,6 +1600,7 @@ fc_status fc_sample_tokens(int32_t dtype, const void *logits, int64_t ld, int32_
         if (!(min_p >= 0.f && min_p <= 1.f)) return fail(FC_ERR_INVALID_ARG, "min_p must be in [0, 1]");
     }
     if (M > 65535 || V > (1 << 24)) return fail(FC_ERR_UNSUPPORTED, "M is limited to 65535, V to 2^24");
+    if ((int64_t)M * V > ((int64_t)1 << 36)) return fail(FC_ERR_UNSUPPORTED, "M * V is limited to 2^36");
     if ((uintptr_t)workspace & 15) return fail(FC_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
     const size_t need = fc_sample_workspace(dtype, M, V), given = workspace ? workspace_bytes : 0;
     if (given < need) return fail(FC_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, given);

@@ -335,9 +335,8 @@ struct PickShared {
     double cum[BINS];       // running sums of weights over the bins, from the largest logit down, in units of 2^-32 of bin 0's upper edge
     double factor[BINS];    // exp(-bin / 32)
     uint32_t count[BINS];   // running counts
-    uint64_t sum[BINS];     // the bins' own sums
     uint64_t list[CAP];     // ranks
-    uint64_t own[PICK];
+    uint64_t own[PICK];     // those of one bin, one a thread
     double wave_sum[PICK / 64];
     uint32_t wave_count[PICK / 64];
     uint64_t digit_sum[256];
@@ -651,7 +650,6 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
         s.wave_sum[tid / 64] = cum;
         s.wave_count[tid / 64] = counts;
     }
-    s.sum[tid] = sum;
     s.factor[tid] = factor;
     if (tid == 0) s.n = 0;
     __syncthreads();

@@ -66,3 +66,25 @@ def test_a_plan_never_exceeds_the_workspace_it_says(knob):
             torch.cuda.synchronize()
             assert bool((ws[room:] == 171).all())
             assert np.isfinite(ref.f64(out)).all()
+
+
+def test_keys_beyond_2_to_the_31_bytes():
+    """2^24 rows of which the last hundred are stored: places of their tiles pass 31 bits.  The others are zeros: score 0, value 0."""
+    S, Dh, A = 1 << 24, 128, 3
+    c = Cache("bf16", 1, 2, 1, Dh, S)
+    q = inputs.normal(40, "q", (1, 2, A, Dh), 1.0, "bf16")
+    k, v = c.rows(41, 100)
+    k = (0.1 * k.float() + 0.5 * q[0, 0, 0].float() + 0.5 * q[0, 1, 1].float()).to(k.dtype)
+    c.store(k, v, start=S - 100)
+    hk, hv = ref.held_rows(ref.f64(k), ref.f64(v))
+    s = np.einsum("had,kd->hak", ref.f64(q)[0], hk[0, 0]) * Dh ** -0.5
+    top = np.maximum(s.max(-1, keepdims=True), 0)
+    w = np.exp(s - top)
+    total = w.sum(-1, keepdims=True) + (S - 100) * np.exp(-top)
+    want = (w / total @ hv[0, 0]).transpose(1, 0, 2)[None]
+    got = c.attend(q, S)
+    # bf16 out, 2^-8; weights 2^-11; scores of at most 50 in magnitude by 2 * 132 roundings of 2^-24; sums of 2^24 weights in fp32: four lanes by four
+    # waves by 64 ranges have 2^14 each, a rounding of 2^-24 every one, and the merges
+    bound = 2.0 ** -8 * np.abs(want) + (2.0 ** -11 + 264 * 50 * 2.0 ** -24 + (2.0 ** 14 + 100) * 2.0 ** -24) * ((w / total) @ np.abs(hv[0, 0])).transpose(1, 0, 2)[None] + 1e-9
+    assert (np.abs(got - want) <= bound).all(), float((np.abs(got - want) - bound).max())
+    assert np.abs(want[0, 0, 0]).max() > 1e-7

@@ -94,6 +94,9 @@ def test_attention_refusals(q4):
     _raises(fc.FC_ERR_BOUNDS, A, q4, 0, FAKE, 4, 301, None, None, FAKE, FAKE, 1 << 30, 0)
     _raises(fc.FC_ERR_INVALID_ARG, A, q4, 0, FAKE, 4, 100, None, None, FAKE, FAKE + 4, 1 << 30, 0)
     _raises(fc.FC_ERR_UNSUPPORTED, A, q4, 0, FAKE, 1 << 24, 100, None, None, FAKE, FAKE, 1 << 30, 0)
+    many = fc.fc_q4_alloc(_cfg(batch=1, n_q_heads=64, n_kv_heads=1), FAKE)
+    _raises(fc.FC_ERR_UNSUPPORTED, A, many, 0, FAKE, (1 << 18) + 1, 100, None, None, FAKE, FAKE, 1 << 30, 0)
+    fc.fc_q4_free(many)
     assert fc.fc_q4_workspace_bytes(_cfg(), 0) == 0 and fc.fc_q4_workspace_bytes(_cfg(head_dim=96), 4) == 0
 
 
@@ -107,6 +110,7 @@ def test_sampling_refusals():
     _raises(fc.FC_ERR_UNSUPPORTED, fc.fc_sample_tokens, **{**good, "V": (1 << 24) + 1, "ld": 1 << 25})
     _raises(fc.FC_ERR_UNSUPPORTED, fc.fc_sample_tokens, **{**good, "M": (1 << 24) + 1})
     assert fc.lib().fc_sample_tokens(7, FAKE, 8, 1, 8, 1.0, 0, 1.0, 0.0, FAKE, FAKE, FAKE, FAKE, 1 << 40, 0) == fc.FC_ERR_INVALID_ARG
+    _raises(fc.FC_ERR_UNSUPPORTED, fc.fc_sample_tokens, **{**good, "M": 65535, "V": 1 << 21, "ld": 1 << 21})
     assert fc.fc_sample_workspace_bytes("bf16", 0, 10) == 0 and fc.fc_sample_workspace_bytes("bf16", 4, 0) == 0
     need = fc.fc_sample_workspace_bytes("bf16", 4, 1000)
     if need:
