@@ -7,11 +7,12 @@
 //  1. k_sample_bins.  Bins of 1/32 of the temperature, on a grid that does not depend on the row: a logit z is in bin floor(32 z / T), its weight
 //     over that of the bin's upper edge lies in (0.969, 1] and is held as a whole number of 2^-32.  Each part of a row counts its entries
 //     and adds their weights up by bins, 1024 of them down from the part's largest; what is further below weighs less than e^-32.
-//  2. k_sample_pick, one workgroup per row.  The parts' bins are added, and running sums over the bins (fp64) say in which bins the targets
-//     lie: the entries of those alone, some hundred of 152064, are fetched, and the targets are found among them by digits of their bits.
+//  2. k_sample_pick, a workgroup per row.  The parts' bins are added, and running sums over the bins (fp64) say in which bins the targets
+//     lie: the entries of those alone, some hundred of 152064, are fetched, from what the parts listed or (by several workgroups where the row is
+//     long) from the row, and the targets are found among them by digits of their bits.
 //
 // Whole sums do not depend on the order in which they are made, so a row gives the same bits whatever else is in the batch and however it is
-// cut.  Weights are exact to 2^-33 and their bins' factors to 2^-53: with sums in fp32, undecided rows would get another token once in a
+// cut.  Weights are exact to 2^-33 and their bins' factors to 2^-50: with sums in fp32, undecided rows would get another token once in a
 // hundred.
 #include <math.h>
 
@@ -200,7 +201,7 @@ template <typename T, int PART>
 __global__ __launch_bounds__(SCAN) void k_sample_bins(FcSampleArgs p, int parts, uint64_t *__restrict__ bins, uint64_t *__restrict__ list,
                                                       Part *__restrict__ about, unsigned long long *__restrict__ shared)
 {
-    constexpr int N = Piece<T>::N, PIECES = PART / (SCAN * N);  // (U pieces are eight values)
+    constexpr int N = Piece<T>::N, PIECES = PART / (SCAN * N);
     __shared__ unsigned long long s_bin[BINS];
     __shared__ uint32_t s_count[BINS], s_wave[SCAN / 64], s_n, s_pieces;
     __shared__ float s_max[SCAN / 64];
@@ -377,9 +378,7 @@ __device__ Found select(PickShared &s, bool counting, uint32_t n, uint64_t targe
 #pragma unroll 1
     while (n > FEW) {
         __syncthreads();
-        if (tid == 0) {
-            s.ones = s.zeros = 0;
-        }
+        if (tid == 0) s.ones = s.zeros = 0;
         if (tid < 256) {
             s.digit_sum[tid] = 0;
             s.digit_count[tid] = 0;
@@ -474,7 +473,7 @@ __device__ Found select(PickShared &s, bool counting, uint32_t n, uint64_t targe
 }
 
 // What select() finds, in one wave without a barrier: entries of bin b in the list, FEW at most.
-__device__ __attribute__((noinline)) Found select_few(PickShared &s, bool counting, const Grid &g, int listed, int b, uint64_t target)
+__device__ __attribute__((noinline)) Found select_few(PickShared &s, bool counting, const Grid g, int listed, int b, uint64_t target)
 {
     const int lane = threadIdx.x;
     const float low = g.lowest(b), high = g.highest(b);
@@ -505,7 +504,7 @@ __device__ __attribute__((noinline)) Found select_few(PickShared &s, bool counti
 }
 
 // The entries of bin b in the list, PICK at most: one a thread.
-__device__ __attribute__((noinline)) Found select_one_each(PickShared &s, bool counting, const Grid &g, int listed, int b, uint64_t target)
+__device__ __attribute__((noinline)) Found select_one_each(PickShared &s, bool counting, const Grid g, int listed, int b, uint64_t target)
 {
     const float low = g.lowest(b), high = g.highest(b);
     double within;
@@ -532,7 +531,7 @@ __device__ __attribute__((noinline)) Found select_one_each(PickShared &s, bool c
 
 // The entries of bin b, n of them, in the list or (LIST false) in the row.
 template <typename T, bool LIST>
-__device__ __attribute__((noinline)) Found select_in(PickShared &s, bool counting, const T *z, int V, const Grid &g, int listed, int b, uint32_t n, uint64_t target)
+__device__ __attribute__((noinline)) Found select_in(PickShared &s, bool counting, const T *z, int V, const Grid g, int listed, int b, uint32_t n, uint64_t target)
 {
     const float low = g.lowest(b), high = g.highest(b);
     return select(s, counting, n, target, [&](auto f) {
@@ -555,7 +554,7 @@ __device__ __attribute__((noinline)) Found select_in(PickShared &s, bool countin
 // Entries [from, to) of a row with logits in one of n ranges: to the list, as far as there is room.  64 values of a thread are in flight together;
 // the few that are wanted are read again.
 template <typename T>
-__device__ __attribute__((noinline)) void fetch(PickShared &s, const T *z, int from, int to, int n, float least0, float most0, float least1, float most1,
+__device__ __forceinline__ void fetch(PickShared &s, const T *z, int from, int to, int n, float least0, float most0, float least1, float most1,
                                                 float least2, float most2)
 {
     constexpr int N = Piece<T>::N, U = 64 / N;
@@ -585,6 +584,13 @@ __device__ __attribute__((noinline)) void fetch(PickShared &s, const T *z, int f
             if (at < CAP) s.list[at] = rank_of(fc_to_float(z[i]), (uint32_t)i);
         }
     }
+}
+
+// Those of one range.  (Apart from the kernel, since it is rare; what is not is in it, as a call saves registers in memory.)
+template <typename T>
+__device__ __attribute__((noinline)) void fetch_range(PickShared &s, const T *z, int V, float least, float most)
+{
+    fetch(s, z, 0, V, 1, least, most, 0.f, 0.f, 0.f, 0.f);
 }
 
 template <typename T>
@@ -766,7 +772,7 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
             const uint32_t at = (uint32_t)s.shared;
             for (uint32_t i = tid; i < own && at + i < (uint32_t)CAP; i += PICK)
                 __hip_atomic_store(&of_all[at + i], s.list[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            __builtin_amdgcn_s_waitcnt(0);
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
             __syncthreads();
             if (tid == 0) s.shared = atomicAdd(&shared[row], 1ull << 32);
             __syncthreads();
@@ -794,7 +800,7 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
         __syncthreads();
         if (tid == 0) s.n = 0;
         __syncthreads();
-        fetch(s, z, 0, p.V, 1, g.lowest(b), g.highest(b), 0.f, 0.f, 0.f, 0.f);
+        fetch_range(s, z, p.V, g.lowest(b), g.highest(b));
         __syncthreads();
         const uint32_t all_in = s.n;
         return all_in <= (uint32_t)CAP ? select_in<T, true>(s, counting, z, p.V, g, (int)all_in, b, n, target)
