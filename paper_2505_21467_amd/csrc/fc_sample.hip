@@ -29,6 +29,7 @@ constexpr int PICK = 1024;                   // threads of the second kernel, on
 constexpr int CAP = 12288;                   // entries that it fetches into LDS
 constexpr int LISTED = 256, LIST = 1024;     // entries that a part lists, about, and at most
 constexpr int FEW = 64;                      // entries that one wave compares with one another
+constexpr int ROOM = BINS + 1;               // bins of a part in memory: the one behind its last is 0
 constexpr int SUM_BITS = 48;
 
 // exp(-i) and exp(-i / 32): a bin's factor is a product of two.  (The library's function costs 2 us here, most of it for code that is not in the
@@ -315,7 +316,7 @@ __global__ __launch_bounds__(SCAN) void k_sample_bins(FcSampleArgs p, int parts,
         }
     }
     __syncthreads();
-    for (int i = tid; i <= last; i += SCAN) bins[at * BINS + i] = s_bin[i];
+    for (int i = tid; i <= last + 1; i += SCAN) bins[at * ROOM + i] = i <= last ? s_bin[i] : 0;
     if (tid == 0 && part == 0) shared[row] = 0;
     if (tid == 0) about[at] = Part{top, s_n <= LIST ? end : -1, min(s_n, (uint32_t)LIST), last};
 }
@@ -551,13 +552,13 @@ __device__ __attribute__((noinline)) Found select_in(PickShared &s, bool countin
     });
 }
 
-// Entries [from, to) of a row with logits in one of n ranges: to the list, as far as there is room.  64 values of a thread are in flight together;
+// Entries [from, to) of a row with logits in one of n ranges: to the list, as far as there is room.  32 values of a thread are in flight together;
 // the few that are wanted are read again.
 template <typename T>
 __device__ __forceinline__ void fetch(PickShared &s, const T *z, int from, int to, int n, float least0, float most0, float least1, float most1,
                                                 float least2, float most2)
 {
-    constexpr int N = Piece<T>::N, U = 64 / N;
+    constexpr int N = Piece<T>::N, U = 32 / N;
     if (to < N) {  // a row of a few entries
         if ((int)threadIdx.x < to) s.list[atomicAdd(&s.n, 1u)] = rank_of(fc_to_float(z[threadIdx.x]), threadIdx.x);
         return;
@@ -567,17 +568,16 @@ __device__ __forceinline__ void fetch(PickShared &s, const T *z, int from, int t
         Piece<T> x[U];
 #pragma unroll
         for (int k = 0; k < U; ++k) x[k] = __builtin_bit_cast(Piece<T>, fc_load_any<uint4>(z + min(i0 + k * PICK * N, to - N)));
-        uint32_t in[2] = {};
+        uint32_t left = 0;
 #pragma unroll 1
         for (int r = 0; r < n; ++r) {
             const float least = r == 0 ? least0 : r == 1 ? least1 : least2, most = r == 0 ? most0 : r == 1 ? most1 : most2;
 #pragma unroll
-            for (int k = 0; k < U * N; ++k) in[k / 32] |= x[k / N].get(k % N) >= least && x[k / N].get(k % N) <= most ? 1u << (k % 32) : 0;
+            for (int k = 0; k < U * N; ++k) left |= x[k / N].get(k % N) >= least && x[k / N].get(k % N) <= most ? 1u << k : 0;
         }
-        uint64_t left = (uint64_t)in[1] << 32 | in[0];
 #pragma unroll 1
         while (left) {
-            const int k = __builtin_ctzll(left), i1 = i0 + k / N * (PICK * N), i = min(i1, to - N) + k % N;
+            const int k = __builtin_ctz(left), i1 = i0 + k / N * (PICK * N), i = min(i1, to - N) + k % N;
             left &= left - 1;
             if (i < i1) continue;  // (of the last 16 bytes, what another piece has)
             const uint32_t at = atomicAdd(&s.n, 1u);
@@ -601,7 +601,7 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
     const int tid = threadIdx.x, row = blockIdx.x, slices = gridDim.y, slice = blockIdx.y;
     const T *z = (const T *)p.logits + (size_t)row * p.ld;
     const Part *about = abouts + (size_t)row * parts;
-    const uint64_t *part = bins + (size_t)row * parts * BINS, *lst = lists + (size_t)row * parts * LIST;
+    const uint64_t *part = bins + (size_t)row * parts * ROOM, *lst = lists + (size_t)row * parts * LIST;
 
     const double factor = FACTORS.whole[tid / PER_T] * FACTORS.part[tid % PER_T];
     float z_max = -__builtin_inff();
@@ -617,9 +617,11 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
     }
     const Grid g(z_max, p.inv_t * PER_T, p.bin_width);
 
-    // Thread i: bin i of the row, eight parts in flight together.  (lists_to: the last bin of which the parts' lists have every entry.)
+    // Thread i: bin i of the row, nine parts in flight together.  (lists_to: the last bin of which the parts' lists have every entry.)
     uint32_t count = 0;
+    static_assert(3 * LONG < 1 << (64 - SUM_BITS) && 32 + 16 <= SUM_BITS, "three parts together");
     uint64_t sum = 0;
+    uint32_t listed_in = 0;  // (lane: of up to 64 parts)
     int lists_to = BINS;
 #pragma unroll 1
     for (int i0 = 0; i0 < parts; i0 += 64) {
@@ -627,24 +629,24 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
         double within;
         const int mine = i0 + tid % 64;
         const Part a = about[min(mine, parts - 1)];
+        listed_in = a.n;
         const int off = mine < parts ? g.bin(a.largest, within) : BINS;
         lists_to = min(lists_to, off < BINS ? (a.bin < 0 ? -1 : off + a.bin) : BINS);
         const int m = min(parts - i0, 64);
 #pragma unroll 1
-        for (int i = 0; i < m; i += 8) {
-            uint64_t x[8];
-            int at[8], last[8];
+        for (int i = 0; i < m; i += 9) {
+            uint64_t x[9];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const int from = min(i + k, m - 1);
-                at[k] = i + k < m ? tid - __builtin_amdgcn_readlane(off, from) : -1;
-                last[k] = __builtin_amdgcn_readlane(a.last, from);
-                x[k] = part[(size_t)(i0 + from) * BINS + max(min(at[k], last[k]), 0)];
+            for (int k = 0; k < 9; ++k) {
+                const int from = min(i + k, m - 1), first = i + k < m ? __builtin_amdgcn_readlane(off, from) : BINS;
+                const uint32_t behind = (uint32_t)__builtin_amdgcn_readlane(a.last, from) + 1;
+                x[k] = (part + (size_t)(i0 + from) * ROOM)[min((uint32_t)(tid - first), behind)];
             }
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                count += at[k] >= 0 && at[k] <= last[k] ? (uint32_t)(x[k] >> SUM_BITS) : 0;
-                sum += at[k] >= 0 && at[k] <= last[k] ? x[k] & ((1ull << SUM_BITS) - 1) : 0;
+            for (int k = 0; k < 9; k += 3) {  // (three parts' counts fit 16 bits, and their sums 48)
+                const uint64_t y = x[k] + x[k + 1] + x[k + 2];
+                count += (uint32_t)(y >> SUM_BITS);
+                sum += y & ((1ull << SUM_BITS) - 1);
             }
         }
     }
@@ -716,13 +718,18 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
         const bool apart = s.count[final] - counted(first) > CAP / 2;
         auto entries = [&](int b0, int b1) { return b0 <= b1 && b1 < BINS ? s.count[b1] - counted(b0) : 0u; };
         if (tid == 0) {
-            Aim a{kb, mb, pb0, pb1, sb0, sb1, final, apart ? 3 : 1, {}, {}, false, false};
+            const float none = __builtin_inff();
+            Aim a{kb, mb, pb0, pb1, sb0, sb1, final, 1, {0.f, none, none}, {0.f, -none, -none}, false, false};
             a.least[0] = g.lowest(apart ? sb1 : final);
             a.most[0] = g.highest(apart ? sb0 : first);
-            a.least[1] = f1 >= 0 ? g.lowest(f1) : __builtin_inff();
-            a.most[1] = f1 >= 0 ? g.highest(f0) : -__builtin_inff();
-            a.least[2] = kb < BINS ? g.lowest(kb) : __builtin_inff();
-            a.most[2] = kb < BINS ? g.highest(kb) : -__builtin_inff();
+            auto add = [&](int b0, int b1) {
+                const float least = g.lowest(b1), most = g.highest(b0);
+                if (a.ranges == 1) a.least[1] = least, a.most[1] = most;
+                else a.least[2] = least, a.most[2] = most;
+                ++a.ranges;
+            };
+            if (apart && f1 >= 0) add(f0, f1);
+            if (apart && kb < BINS) add(kb, kb);
             // (too many for the list: bin by bin, then)
             a.by_bin = (apart ? entries(sb0, sb1) + entries(f0, f1) + entries(kb, kb) : entries(first, final)) > (uint32_t)CAP;
             a.few = max(max(entries(kb, kb), entries(mb, mb)), max(entries(pb0, pb1), entries(sb0, sb1))) <= (uint32_t)FEW;
@@ -741,8 +748,8 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
     if (listed_all) {  // a wave to a part
         if (slice) return;
 #pragma unroll 1
-        for (int i = tid / 64; i < parts; i += PICK / 64) {
-            const uint32_t n = about[i].n;
+        for (int i = __builtin_amdgcn_readfirstlane(tid / 64); i < parts; i += PICK / 64) {
+            const uint32_t n = parts <= 64 ? (uint32_t)__builtin_amdgcn_readlane((int)listed_in, i) : about[i].n;
 #pragma unroll 1
             for (uint32_t j0 = tid % 64; j0 < n; j0 += 4 * 64) {
                 uint64_t r[4];
@@ -872,7 +879,7 @@ struct Plan {
         const int most = row < 256 << 10 ? 1 : (int)(row / SLICE);
         if (slices > most) slices = most;
         const size_t n = (size_t)M * parts;
-        lists = align256(n * BINS * sizeof(uint64_t));
+        lists = align256(n * ROOM * sizeof(uint64_t));
         abouts = lists + align256(n * LIST * sizeof(uint64_t));
         shared = abouts + align256(n * sizeof(Part));
         fetched = shared + align256((size_t)M * sizeof(uint64_t));
