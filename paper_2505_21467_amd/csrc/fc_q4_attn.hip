@@ -473,7 +473,8 @@ void launch(const AttnArgs &p, const FcQ4Plan &pl, hipStream_t s)
 {
     constexpr int RT = MOST_RT<T>;
     if (pl.rt == 2) pl.waves == 8 ? launch_w<T, DH, RT, 8>(p, s) : launch_w<T, DH, RT, 4>(p, s);
-    else pl.waves == 8 ? launch_w<T, DH, 1, 8>(p, s) : launch_w<T, DH, 1, 4>(p, s);
+    else if (pl.waves > 2) pl.waves == 8 ? launch_w<T, DH, 1, 8>(p, s) : launch_w<T, DH, 1, 4>(p, s);
+    else pl.waves == 2 ? launch_w<T, DH, 1, 2>(p, s) : launch_w<T, DH, 1, 1>(p, s);
     if (p.splits > 1) k_q4_merge<T, DH><<<dim3((unsigned)((p.rows + 1024 / DH - 1) / (1024 / DH)), (unsigned)(p.units / p.splits)), dim3(256), 0, s>>>(p);
 }
 
@@ -495,19 +496,24 @@ struct Q4Shape {
     int rt, waves;
     double start, wave, unit, wg, merge, range, mb, part;
 };
-const Q4Shape Q4_128[] = {{1, 4, 4.06, 0.650, 0.157, 0.65, 2.28, 0.077, 0.372, 0.59},
-                          {1, 8, 3.47, 1.047, 0.158, 2.14, 2.10, 0.076, 0.434, 0.75},
-                          {2, 4, 4.87, 0.920, 0.235, 1.43, 2.26, 0.087, 0.312, 0.70},
-                          {2, 8, 4.11, 1.588, 0.244, 2.84, 2.19, 0.082, 0.386, 1.0}};
-const Q4Shape Q4_64[] = {{1, 4, 3.77, 0.476, 0.098, 0.25, 2.13, 0.085, 0.404, 1.0},
-                         {1, 8, 3.61, 0.757, 0.094, 0.74, 2.13, 0.082, 0.516, 0.65},
-                         {2, 4, 4.49, 0.694, 0.161, 0.0, 2.05, 0.088, 0.606, 0.88},
-                         {2, 8, 3.85, 1.161, 0.167, 0.98, 2.14, 0.066, 1.002, 0.92}};
+const Q4Shape Q4_128[] = {{1, 1, 4.84, 0.614, 0.173, 0.34, 1.81, 0.072, 0.387, 0.50},
+                          {1, 2, 4.31, 0.638, 0.174, 0.45, 2.14, 0.075, 0.299, 1.0},
+                          {1, 4, 4.10, 0.642, 0.149, 0.79, 2.18, 0.074, 0.318, 0.46},
+                          {1, 8, 3.50, 1.049, 0.157, 2.24, 2.01, 0.073, 0.373, 0.66},
+                          {2, 4, 4.89, 0.914, 0.237, 1.52, 2.14, 0.084, 0.303, 0.59},
+                          {2, 8, 4.10, 1.596, 0.243, 2.84, 2.00, 0.081, 0.408, 1.0}};
+const Q4Shape Q4_64[] = {{1, 1, 4.07, 0.460, 0.117, 0.25, 1.91, 0.079, 0.461, 0.35},
+                         {1, 2, 3.81, 0.482, 0.107, 0.33, 2.08, 0.082, 0.398, 0.89},
+                         {1, 4, 3.70, 0.490, 0.090, 0.44, 2.18, 0.079, 0.353, 0.66},
+                         {1, 8, 3.53, 0.773, 0.085, 1.11, 2.19, 0.068, 0.329, 0.51},
+                         {2, 4, 4.29, 0.708, 0.137, 0.68, 2.23, 0.070, 0.469, 1.0},
+                         {2, 8, 3.64, 1.154, 0.154, 2.04, 2.36, 0.046, 0.657, 0.76}};
 
 // Estimated time of a call: the longest of a wave's chain of tiles, a compute unit's tiles and the stream from HBM, joined by a 4-norm, and the rest.
-// The load of a compute unit is that of the die with the most units.  Fitted to 2344 measured (shape, plan) pairs of 110 shapes (1 .. 8 sequences, 1 ..
-// 32 kv heads, 1 .. 8 query heads each, 1 .. 256 rows, 16 .. 16800 keys from HBM; rms error 4 .. 8 %); the plan it picks is 1.2 %
-// slower than the best measured one in the mean, 13 % at most.
+// The load of a compute unit is that of the die with the most units.  Fitted to 4068 measured (shape, plan) pairs of 160 shapes (1 .. 8 sequences, 1 ..
+// 32 kv heads, 1 .. 8 query heads each, 1 .. 256 rows, 8 .. 16800 keys from HBM; rms error 4 .. 9 %); the plan it picks is 1.4 %
+// slower than the best measured one in the mean, 14 % at most.  One wave and two are for few keys and many rows: 4 sequences, 8 kv heads of 7, 160
+// rows, 32 keys take 10.1 us with one, 14.5 with four; 8 sequences, 28 / 4 heads, 256 rows, 128 keys 16.5 and 23.2.
 double q4_cost(const Q4Shape &sh, int64_t pairs, int64_t rows, int64_t tiles, int dh, int64_t splits)
 {
     const int64_t groups = (rows + 16 * sh.rt - 1) / (16 * sh.rt), per = (tiles + splits - 1) / splits;
@@ -530,7 +536,9 @@ FcQ4Plan plan(const FcQ4Geom &G, int A, int kv_len, size_t cap)
     FcQ4Plan best{1, 4, 1};
     const FcKnobs &k = fc_knobs();
     if (k.q4_rt > 0) {  // a tuning knob asks for one
-        best = FcQ4Plan{k.q4_rt == 2 && G.dtype != FC_F32 ? 2 : 1, k.q4_waves == 8 ? 8 : 4, k.q4_splits > 0 ? k.q4_splits : 1};
+        best.rt = k.q4_rt == 2 && G.dtype != FC_F32 ? 2 : 1;
+        best.waves = k.q4_waves == 8 || (best.rt == 1 && (k.q4_waves == 1 || k.q4_waves == 2)) ? k.q4_waves : 4;
+        best.splits = k.q4_splits > 0 ? k.q4_splits : 1;
         if (best.splits > tiles) best.splits = (int)tiles;
         while (best.splits > 1 && fc_q4_plan_workspace(G, best, A) > cap) --best.splits;
         return best;

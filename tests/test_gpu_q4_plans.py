@@ -13,7 +13,7 @@ pytestmark = pytest.mark.gpu
 
 
 @pytest.mark.parametrize("dtype,Dh", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
-@pytest.mark.parametrize("tiles,waves", [(1, 4), (1, 8), (2, 4), (2, 8)])
+@pytest.mark.parametrize("tiles,waves", [(1, 1), (1, 2), (1, 4), (1, 8), (2, 4), (2, 8)])
 def test_every_plan(knob, dtype, Dh, tiles, waves):
     """37 rows of a kv head (a last row tile that is not full), 20 tiles of keys of which the last is not full; lengths of which some leave
     ranges, or all but a wave, without keys; rows that are padding."""
