@@ -858,10 +858,10 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
 // How a call is cut.  Parts are as short as leaves a row 20 of them (the second kernel adds them up) and the call 384 workgroups of parts twice as
-// long: 32 x 152064 take 31.8 us by parts of 8192, 32.7 by 16384 and 37.8 by 4096, one row of 32000 24.0 by 4096 and 27.1 by 8192, 400 x 9001 74.9 by
-// 16384 and 78.6 by 8192.  Where a row's lists do not do, rows of 256 KB and more are fetched by as many workgroups as there are compute units to a
-// row, of SLICE bytes at least: the handing over takes 4 us (57 rows of 50001 fp32: 32.4 us with one workgroup, 36.7 with two), and a workgroup
-// reads 20 GB/s (32 x 152064 fp32: 70 us with one, 58 with six; 8 x 152064 bf16 42.6 with one, 37.2 with three).
+// long: 32 x 152064 take 27.5 us by parts of 8192, 28.2 by 16384 and 32.1 by 4096; one row of 32000 without filters 17.0 by 4096, 19.4 by 8192 and
+// 24.3 by 16384; 256 x 152064 42.5 by 16384 and 51.6 by 8192.  Where a row's lists do not do, rows of 256 KB and more are fetched by as many
+// workgroups as there are compute units to a row, of SLICE bytes at least, which costs them a ticket (57 rows of 50001 fp32: 27.1 us with one
+// workgroup, 27.6 with two; 32 x 152064 fp32: 48.2 with one, 39.8 with six; 8 x 152064 bf16 33.6 with one, 30.3 with three).
 // The workspace has the parts' bins, their lists, what is said about them, and what the slices fetch.
 struct Plan {
     int part, parts, slices;
