@@ -370,7 +370,8 @@ __device__ __forceinline__ void before_own(const Entry &own, uint32_t n, uint64_
 
 // Among the n entries that each(f) calls f(rank, weight) for: the one at which the running count or sum, larger ranks first, passes
 // `target`; the last one if none does.  Digits of 8 bits from the first bit in which the ranks differ, until a wave can compare what is left.
-template <typename EACH>
+// ROW: entries come in the order of their index.
+template <bool ROW, typename EACH>
 __device__ Found select(PickShared &s, bool counting, uint32_t n, uint64_t target, EACH each)
 {
     const int tid = threadIdx.x;
@@ -404,8 +405,19 @@ __device__ Found select(PickShared &s, bool counting, uint32_t n, uint64_t targe
         each([&](uint64_t rank, uint64_t w) {
             if (rank < low || rank > high) return;
             const uint32_t d = (uint32_t)(rank >> shift) & mask;
-            atomicAdd((unsigned long long *)&s.digit_sum[d], (unsigned long long)w);
-            atomicAdd(&s.digit_count[d], 1u);
+            uint32_t n = 1;
+            if constexpr (ROW) {
+                // (equal entries next to one another have one digit and one weight: one addition for all lanes, where 64 to one place took twice the time)
+                const uint64_t lanes = __ballot(true);
+                const uint32_t d0 = (uint32_t)__builtin_amdgcn_readfirstlane((int)d);
+                const uint64_t w0 = of_lane(w, (uint32_t)__builtin_ctzll(lanes));
+                if (__ballot(d == d0 && w == w0) == lanes) {
+                    if (tid % 64 != __builtin_ctzll(lanes)) return;
+                    n = (uint32_t)__builtin_popcountll(lanes);
+                }
+            }
+            atomicAdd((unsigned long long *)&s.digit_sum[d], (unsigned long long)(w * n));
+            atomicAdd(&s.digit_count[d], n);
         });
         __syncthreads();
         if (tid < 64) {  // lane i has the digits 255 - 4 i .. 252 - 4 i
@@ -525,7 +537,7 @@ __device__ __attribute__((noinline)) Found select_one_each(PickShared &s, bool c
     const uint64_t rank = s.own[threadIdx.x];
     g.bin(logit_of(rank), within);
     const uint64_t weight = g.weight(within);
-    return select(s, counting, n, target, [&](auto f) {
+    return select<false>(s, counting, n, target, [&](auto f) {
         if (threadIdx.x < n) f(rank, weight);
     });
 }
@@ -535,7 +547,7 @@ template <typename T, bool LIST>
 __device__ __attribute__((noinline)) Found select_in(PickShared &s, bool counting, const T *z, int V, const Grid g, int listed, int b, uint32_t n, uint64_t target)
 {
     const float low = g.lowest(b), high = g.highest(b);
-    return select(s, counting, n, target, [&](auto f) {
+    return select<!LIST>(s, counting, n, target, [&](auto f) {
         double within;
         if constexpr (LIST) {
 #pragma unroll 1
@@ -804,6 +816,7 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
         if (alone) return select_few(s, counting, g, listed, b, target);
         const uint32_t n = s.count[b] - counted(b);
         if (list) return n <= PICK ? select_one_each(s, counting, g, listed, b, target) : select_in<T, true>(s, counting, z, p.V, g, listed, b, n, target);
+        if (n > (uint32_t)CAP) return select_in<T, false>(s, counting, z, p.V, g, 0, b, n, target);
         __syncthreads();
         if (tid == 0) s.n = 0;
         __syncthreads();
