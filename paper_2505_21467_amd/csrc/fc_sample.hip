@@ -197,7 +197,8 @@ struct __align__(16) Part {
 // One part of a row: bins[] gets (entries << 48 | sum of weights), list[] the ranks of some 256 of its largest entries.
 //
 // The largest entries of the threads' pieces say where to end: at least as many entries as pieces reach a bin, so with a top-k nothing below the
-// bin that k pieces reach can be kept, and is not weighed; the list ends at the bin that 256 reach.
+// bin that k pieces reach can be kept, and is not weighed; the list ends at the bin that 256 reach, or twice
+// this part's share of the top-k.
 template <typename T, int PART>
 __global__ __launch_bounds__(SCAN) void k_sample_bins(FcSampleArgs p, int parts, uint64_t *__restrict__ bins, uint64_t *__restrict__ list,
                                                       Part *__restrict__ about, unsigned long long *__restrict__ shared)
@@ -256,7 +257,7 @@ __global__ __launch_bounds__(SCAN) void k_sample_bins(FcSampleArgs p, int parts,
         if (tid % 64 == 63) s_wave[tid / 64] = run;
         __syncthreads();
         run += sum_before<SCAN / 64>(s_wave);
-        const uint32_t ks[2] = {p.top_k > 0 ? (uint32_t)p.top_k : 0xffffffffu, (uint32_t)min(max(p.top_k, LISTED), 2 * LISTED)};
+        const uint32_t ks[2] = {p.top_k > 0 ? (uint32_t)p.top_k : 0xffffffffu, (uint32_t)min(max(2 * p.top_k / parts, LISTED), 2 * LISTED)};
 #pragma unroll
         for (int i = 0; i < 2; ++i)
             if (run >= ks[i] && run - a - b < ks[i]) s_last[i] = run - b >= ks[i] ? 2 * tid : 2 * tid + 1;
@@ -723,6 +724,13 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
                 high = fmin(high, s.cum[mb]);
             }
         }
+        // (the shortest prefix counts: a filter that ends in a later bin than another one does need not be looked at, but for the top-k whose sum top-p takes)
+        if (mb < BINS && pb1 >= 0 && mb > pb1) mb = BINS;
+        if (mb < pb0) {
+            pb0 = BINS;
+            pb1 = -1;
+        }
+        if (pb1 < 0 && mb < kb) kb = BINS;
         const int sb0 = token_bin(low), sb1 = low < high ? token_bin(high) : sb0;
         // Logits of the bin in which top-k ends, of those in which the other filters can, and of the token's.  Where they lie apart with many entries
         // between them, three ranges; else one.
@@ -832,7 +840,7 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
         const Found f = pick(true, kb, (uint64_t)p.top_k - counted(kb) - 1);
         total = before(kb) + s.factor[kb] * (double)f.sum;
     }
-    if (p.top_p < 1.f) {
+    if (pb1 >= 0) {
         const double x = (double)p.top_p * total;
         const int b = min(max(reach(x, false), pb0), pb1);
         const double y = ceil((x - before(b)) / s.factor[b]) - 1.;  // a sum that reaches x passes the whole number below it

@@ -85,3 +85,14 @@ def test_nothing_behind_the_workspace_is_touched():
             fc.fc_sample_tokens(dtype, z.to(t).to(DEV), V, M, V, 1.0, f[0], f[1], 0.0, u.to(DEV), tok, conf, ws, bytes_)
             torch.cuda.synchronize()
             assert bool((ws[bytes_:] == 171).all())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_which_filter_ends_first(dtype):
+    """Top-k, top-p and min-p ending far before and behind one another, in every order, and near one another; hardly decided rows and peaked ones."""
+    for peaks in (0.0, 12.0):
+        z, u = _logits(86, 5, 50001, 1.2, peaks=peaks)
+        for k in (0, 3, 600, 20000):
+            for top_p in (1.0, 0.02, 0.5, 0.98):
+                for min_p in (0.0, 0.7, 0.05, 0.0005):
+                    _check(z, dtype, u, what="%s %s %s %s" % (peaks, k, top_p, min_p), top_k=k, top_p=top_p, min_p=min_p, temperature=0.9)
