@@ -317,3 +317,34 @@ def test_rows_beyond_what_a_cache_holds(dtype, Dh, B, rows):
     for a, b in ((0, half), (half, rows)):
         small.store(k[:, :, a:b].contiguous(), v[:, :, a:b].contiguous(), start=5 + a)
     assert torch.equal(c.storage, small.storage)
+
+
+@pytest.mark.parametrize("dtype,Dh", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("from_cache", [False, True])
+def test_few_listed_places_of_a_long_cache(dtype, Dh, from_cache):
+    """Fewer entries than tiles: entries of one tile, apart and next to one another, a place named three times, padding, the last place."""
+    S, B, Hkv = 2000, 2, 3
+    c = Cache(dtype, B, 3, Hkv, Dh, S)
+    k0, v0 = c.rows(25, S)
+    c.store(k0, v0)
+    hk, hv = ref.held_rows(ref.f64(k0), ref.f64(v0))
+    pos = torch.tensor([[70, -1, 1999, 64, 70, 127, 640, 2000, 70, 0, 128], [5, 5, -9, 1990, 4, 6, 2 ** 31 - 1, 1300, 1301, 1299, 5]], dtype=torch.int32)
+    rows = pos.shape[1]
+    if from_cache:
+        full = fc.fc_cache_alloc(fc.make_config(1, B, 256, 3, Hkv, Dh, S, dtype))
+        k, v = c.rows(26, S)
+        fc.fc_cache_write_rows(full, 0, k.to(DEV), v.to(DEV), 0, S)
+        fc.fc_q4_store_from(c.handle, 0, full, 0, pos.to(DEV), 0, rows)
+    else:
+        k, v = c.rows(26, rows, 2.0)
+        c.store(k, v, pos)
+    nk, nv = ref.held_rows(ref.f64(k), ref.f64(v))
+    for b in range(B):
+        for r, p in enumerate(pos[b].tolist()):
+            if 0 <= p < S:
+                hk[b, :, p], hv[b, :, p] = nk[b, :, p if from_cache else r], nv[b, :, p if from_cache else r]
+    gk, gv = c.read()
+    assert np.array_equal(gk, hk) and np.array_equal(gv, hv)
+    if from_cache:
+        torch.cuda.synchronize()
+        fc.fc_cache_free(full)

@@ -96,3 +96,42 @@ def test_which_filter_ends_first(dtype):
             for top_p in (1.0, 0.02, 0.5, 0.98):
                 for min_p in (0.0, 0.7, 0.05, 0.0005):
                     _check(z, dtype, u, what="%s %s %s %s" % (peaks, k, top_p, min_p), top_k=k, top_p=top_p, min_p=min_p, temperature=0.9)
+
+
+@pytest.mark.parametrize("f", [(0, 0.9), (0, 1.0), (40, 0.9)])
+def test_replays_of_a_call_whose_workgroups_wait_for_nobody(f):
+    """Rows that several workgroups fetch, recorded into a graph: other numbers and logits with every replay, over a workspace that was overwritten."""
+    M, V = 2, 152064
+    z = torch.empty((M, V), device=DEV)
+    u, tok, conf = torch.empty(M, device=DEV), torch.empty(M, dtype=torch.int32, device=DEV), torch.empty(M, device=DEV)
+    ws = torch.empty(fc.fc_sample_workspace_bytes("f32", M, V), dtype=torch.uint8, device=DEV)
+    call = lambda: fc.fc_sample_tokens("f32", z, V, M, V, 1.0, f[0], f[1], 0.0, u, tok, conf, ws)
+
+    def fill(seed):
+        a, b = _logits(seed, M, V, 1.0, peaks=0.0)
+        z.copy_(a)
+        u.copy_(b)
+
+    fill(90)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for replay in range(5):
+        fill(91 + replay)
+        ws.fill_(255 if replay % 2 else 1)
+        call()
+        torch.cuda.synchronize()
+        want = tok.clone(), conf.clone()
+        ws.fill_(170)
+        tok.zero_()
+        graph.replay()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(tok, want[0]) and torch.equal(conf, want[1]), replay
+        assert int(tok.min()) >= 0 and int(tok.max()) < V
