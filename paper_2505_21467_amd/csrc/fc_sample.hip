@@ -72,23 +72,24 @@ struct Grid {
     float most;
     bool infinite;  // then the infinite logits are in bin 0, and no others in any
     double c, by_c, top;  // bins to a unit of logit, 1 / that; the largest logit's bin
-    __device__ __forceinline__ Grid(float most_, double c_, double by_c_) : most(most_), infinite(most_ > 3.4028235e38f), c(c_), by_c(by_c_), top(floor((double)most_ * c_)) {}
+    __device__ __forceinline__ Grid(float most_, double c_, double by_c_) : most(most_), infinite(__builtin_amdgcn_readfirstlane(most_ > 3.4028235e38f)), c(c_), by_c(by_c_), top(floor((double)most_ * c_)) {}
     __device__ __forceinline__ int bin(float z, double &within) const
     {
 #pragma clang fp contract(off)  // (x is rounded: with one fused operation for x - b an entry's weight would depend on where it is computed)
         const double x = (double)z * c, b = floor(x);
         within = x - b;
-        const double d = top - b;
         if (infinite) return z == most ? 0 : BINS;
-        return d < (double)BINS ? (int)d : BINS;  // (NaN: none)
+        return (int)fmin(top - b, (double)BINS);  // (NaN: none)
     }
-    // exp((within - 1) / 32) in units of 2^-32: a Taylor series about the middle of the bin, off by less than 2^-45.
+    // exp((within - 1) / 32) in units of 2^-32: with h = 1/64 and |u| <= h, exp(u) by its Taylor series to the fifth power, of which u^5 is given up
+    // for what Chebyshev's polynomial says of it, (20 h^2 u^3 - 5 h^4 u) / 16; off by less than 2^-40.
     __device__ __forceinline__ uint64_t weight(double within) const
     {
         if (infinite) return 1ull << 32;
-        const double u = (within - 0.5) * (1.0 / PER_T);
-        const double e = 1.0 + u * (1.0 + u * (1.0 / 2 + u * (1.0 / 6 + u * (1.0 / 24 + u * (1.0 / 120)))));
-        return (uint64_t)__double_as_longlong(e * (0.98449643700540845 * 4294967296.0) + 4503599627370496.0) & 0xfffffffffffffull;  // exp(-1/64); 2^52 rounds
+        constexpr double h = 0.5 / PER_T;
+        const double u = fma(within, 1.0 / PER_T, -h);
+        const double e = fma(u, fma(u, fma(u, fma(u, 1.0 / 24, 1.0 / 6 + h * h / 96), 1.0 / 2), 1.0 - h * h * h * h / 384), 1.0);
+        return (uint64_t)__double_as_longlong(fma(e, 0.98449643700540845 * 4294967296.0, 4503599627370496.0)) & 0xfffffffffffffull;  // exp(-h); 2^52 rounds
     }
     // Logits of bins b0 .. b1, and perhaps a few more on either side.
     __device__ __forceinline__ float lowest(int b1) const
