@@ -267,21 +267,32 @@ __global__ __launch_bounds__(SCAN) void k_sample_bins(FcSampleArgs p, int parts,
         end = min(last, s_last[1] + 2);
         const float cut = g.lowest(last);
         // Pieces with an entry that matters are listed, spread over the threads and read again: under a top-k of 50 one entry in hundreds does, and every
-        // wave has some.
+        // wave has some.  Those with an entry for the list come first, the others from behind, so that most waves need not ask for places in it.
+        const float first_cut = g.lowest(end);
+        const bool some_others = __builtin_amdgcn_readfirstlane(end < last);  // (under a small top-k all that matters is listed)
 #pragma unroll
         for (int i = 0; i < PIECES; ++i) {
-            const uint64_t in = __ballot(best[i] >= cut);
-            if (!in) continue;
+            const bool first = best[i] >= first_cut;
+            const uint64_t firsts = __ballot(first);
+            bool other = false;
+            uint64_t others = 0;
+            if (some_others) {
+                other = !first && best[i] >= cut;
+                others = __ballot(other);
+            }
+            if (!(firsts | others)) continue;
             uint32_t base = 0;
-            if (tid % 64 == 0) base = atomicAdd(&s_pieces, (uint32_t)__builtin_popcountll(in));
+            if (tid % 64 == 0) base = atomicAdd(&s_pieces, (uint32_t)__builtin_popcountll(others) << 16 | (uint32_t)__builtin_popcountll(firsts));
             base = __builtin_amdgcn_readfirstlane(base);
-            const uint32_t to = __builtin_amdgcn_mbcnt_hi((uint32_t)(in >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in, base));
-            if (best[i] >= cut) s_piece[to] = (uint16_t)(i * SCAN + tid);
+            const uint64_t mine = first ? firsts : others;
+            const uint32_t to = __builtin_amdgcn_mbcnt_hi((uint32_t)(mine >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mine, first ? base & 0xffff : base >> 16));
+            if (first || other) s_piece[first ? to : PIECES * SCAN - 1 - to] = (uint16_t)(i * SCAN + tid);
         }
         __syncthreads();
+        const int firsts = (int)(s_pieces & 0xffff), pieces = firsts + (int)(s_pieces >> 16);
 #pragma unroll 1
-        for (int i = tid; i < (int)s_pieces; i += SCAN) {
-            const int first = from + s_piece[i] * N;
+        for (int i = tid; i < pieces; i += SCAN) {
+            const int first = from + s_piece[i < firsts ? i : PIECES * SCAN - 1 - (i - firsts)] * N;
             Piece<T> x;
             x.load(z, first, to);
             // four entries at a time: their chains of fp64 operations overlap, and the wave takes places in the list for all at once
@@ -301,7 +312,7 @@ __global__ __launch_bounds__(SCAN) void k_sample_bins(FcSampleArgs p, int parts,
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     if (bin[j] <= last) atomicAdd(&s_bin[bin[j]], (unsigned long long)(1ull << SUM_BITS | w[j]));
-                if (n) {
+                if (n && i - tid % 64 < firsts) {
                     const int leader = __builtin_ctzll(__ballot(true));
                     uint32_t place = 0;
                     if (tid % 64 == leader) place = atomicAdd(&s_n, n);
