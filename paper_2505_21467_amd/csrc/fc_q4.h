@@ -1,9 +1,9 @@
 // The cache held in 4 bits: layout of a tile of 64 rows of one (sequence, kv head), shared by the kernels that fill and read it.
 //
-// A tile is one run of bytes: key codes, value codes, key scales, value scales.  Inside it the codes lie as the matrix
-// instructions take them, so that a wave loads its operands with 16 bytes per lane, 1 KB in a piece, and moves nothing
+// A tile is one run of bytes: key codes, value codes, key scales, value scales.  Inside it the codes lie in the lanes that the matrix
+// instructions take their values from, so that a wave loads its operands with 16 bytes per lane, 1 KB in a piece, and moves nothing
 // between lanes:
-//   key codes    [16 rows][block of 32 elements][row] 16 bytes, the operand of a 16x16x128 multiply with block scales
+//   key codes    [16 rows][block of 32 elements][row] 16 bytes: word i of a lane's is its eight elements of the i-th 16x16x32 multiply
 //   value codes  [chunk][lane][4] words: word w = 4 chunk + place is elements 16 (w / 2) .. + 15 of rows 32 (w % 2) .. + 31; the
 //                lane's element is lane % 16, and its eight codes are rows 4 (lane / 16) + {0 .. 3} and the same + 16: the
 //                order in which the lane holds the weights of those rows after the key multiply

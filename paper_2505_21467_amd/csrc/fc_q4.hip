@@ -1,7 +1,7 @@
 // Rows of keys and values held in 4 bits: the tiles they are kept in, storing rows and reading them back.
 //
 // A value is an E2M1 number (0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives) times a power of two: a key row has one power per
-// block of 32 elements, which is what the matrix instructions with block scales take, a value row one for all its elements, which
+// block of 32 elements (channels of very different sizes stay apart), a value row one for all its elements, which
 // the attention multiplies the row's weight by instead of the row.  The power is the least one with which the block's largest
 // magnitude is at most 6, so nothing is clipped, and x 2^-e is exact: the only rounding is the one to E2M1 (nearest, ties to the
 // even code), which makes what is stored the same bits whoever computes it.

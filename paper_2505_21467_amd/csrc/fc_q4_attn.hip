@@ -4,19 +4,20 @@
 // query heads that share a kv head are one list) and takes tiles of 64 keys, straight from memory into operand registers: the
 // tile's layout is the operands' (fc_q4.h), so the main loop has no barrier and, but for 64 scales, no lane crosses.
 //
-//  - Scores.  The 16x16x128 matrix instruction with block scales takes the key codes and their scales as they are stored; with a 6-bit other operand
-//    it takes 16 clocks, a quarter of what bfloat16 products of that size take.  What a query lacks in bits it gets by parts: a lane's 32
-//    elements of a row are three E2M3 numbers each, every one the rounding error of those before, 2^-14 of the largest of the 32 in the
-//    end (the rows are bfloat16).  48 clocks, and no key is ever converted.  (Two e4m3 parts: 64 clocks.)
+//  - Scores.  Key codes become bfloat16 by one conversion for two (a number of the format times its power of two is one, exactly), once for all
+//    RT row tiles, and a bfloat16 row is multiplied as it is: nothing is lost before the sums in fp32, however far the elements of a row
+//    are apart.  (The matrix instructions with block scales take the codes unconverted, but the row then has to go in as 6-bit numbers,
+//    each part 5 bits more below the largest of 32 elements: with three parts, 2^-14, channels 256 times the others cost 3.5e-3 of
+//    the result, and four take as long as the conversions.  As two 8-bit numbers its products would be cut off at 2^-14 of their sum.)
 //  - Weights.  Value row t is codes times 2^e_t.  The power goes into the exponent of the row's weight, w_t = 2^(s_t + e_t - r), so the codes
 //    are multiplied as they are, and the sum that divides adds w_t 2^-e_t.  The key multiply starts from e_t over the softmax scale, so this
 //    costs nothing.  The reference r only has to keep w_t in range: it moves when a score passes it by 2^MOVE, which after the first
 //    tiles is rare.  Weights are rounded to fp16 (11 bits; bfloat16 would add as much error as rounding the output does, two E2M3 parts
 //    more, 2.8e-3 for 1.7e-3 relative in all), sums are fp32.
-//  - fp32 rows have six parts (2^-29 of the largest), and a weight is two fp16 numbers, the second in units of 2^-12 with sums of its own: 2^-23 of
-//    the weight.  The reference is a whole number and e_t - r is added with the scale, so a score is rounded once.  Errors against 64 bits are
-//    1e-7 .. 2e-7, a quarter of a plain fp32 computation's; 1 x 32 rows x 28 heads over 1056 keys take 9.1 us (bfloat16: 6.7; one wave per row
-//    with plain fp32 arithmetic took 46 us for 8 rows x 4 heads over 96 keys, where this takes 4.6).
+//  - fp32 rows are three bfloat16 numbers, 8 bits each, which is all of them, and a weight is two fp16 numbers, the second in units of 2^-12 with sums
+//    of its own: 2^-23 of the weight.  The reference is a whole number and e_t - r is added with the scale, so a score is rounded once.
+//    Errors against 64 bits are 1.6e-7 (heads of 64) and 2.2e-7 (128), less than half of a plain fp32 computation's; 32 rows x 28 heads over
+//    1056 keys take 9.9 us (bfloat16: 6.8).
 //  - Values.  Codes become fp16 pairs by one conversion each, once for all RT row tiles.
 //
 // The waves of a workgroup take tiles in turn and add up in LDS at the end.  Where there are few (sequence, kv head, row group)
@@ -31,14 +32,12 @@
 namespace {
 
 typedef float f4 __attribute__((ext_vector_type(4)));
-typedef float f16x __attribute__((ext_vector_type(16)));
-typedef float f32x __attribute__((ext_vector_type(32)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-typedef int i8x __attribute__((ext_vector_type(8)));
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+typedef __bf16 b2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u6 __attribute__((ext_vector_type(6)));
 
 constexpr float MOVE = 8.f;  // a score may pass the reference by 2^MOVE
 constexpr float FINE = 4096.f;  // fp32: what a weight's fp16 lacks is multiplied in units of 1 / FINE
@@ -58,14 +57,24 @@ struct AttnArgs {
 // What a wave loads of a tile.  Buffer loads: the place of the tile is a scalar, a lane keeps three offsets.
 template <int DH>
 struct Tile {
-    u4 k[4], v[DH / 32];
+    uint32_t k[4][DH / 32];
+    u4 v[DH / 32];
     uint32_t ks, vs;
     __device__ __forceinline__ void load_keys(__amdgpu_buffer_rsrc_t r, uint32_t at, int lane)
     {
-        const int kl = DH == 128 ? lane : lane & 31;  // (heads of 64: the upper lanes multiply the same keys with the second part)
 #pragma unroll
-        for (int t = 0; t < 4; ++t) k[t] = __builtin_amdgcn_raw_buffer_load_b128(r, kl * 16, at + t * (8 * DH), 0);
-        ks = __builtin_amdgcn_raw_buffer_load_b32(r, kl * 4, at + 64 * DH, 0);
+        for (int t = 0; t < 4; ++t) {
+            if constexpr (DH == 128) {
+                const u4 x = __builtin_amdgcn_raw_buffer_load_b128(r, lane * 16, at + t * (8 * DH), 0);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) k[t][i] = x[i];
+            } else {  // (two blocks to a row: the upper lanes have the second half of the lower ones')
+                const u2 x = __builtin_amdgcn_raw_buffer_load_b64(r, (lane & 31) * 16 + (lane >> 5) * 8, at + t * (8 * DH), 0);
+                k[t][0] = x[0];
+                k[t][1] = x[1];
+            }
+        }
+        ks = __builtin_amdgcn_raw_buffer_load_b32(r, (DH == 128 ? lane : lane & 31) * 4, at + 64 * DH, 0);
         vs = __builtin_amdgcn_raw_buffer_load_b32(r, lane & ~3, at + fc_q4_vscale(DH), 0);
     }
     __device__ __forceinline__ void load_values(__amdgpu_buffer_rsrc_t r, uint32_t at, int lane)
@@ -75,116 +84,52 @@ struct Tile {
     }
 };
 
-// 32 values over `scale` as E2M3, and back.  The even ones come from `a`, the odd ones from `b`.  The instruction writes its first results before
-// it has read its last sources and its scale: they are kept alive behind it, so that the compiler gives it other registers.
-__device__ __forceinline__ u6 to_6bit(const f16x &a, const f16x &b, float scale)
+// Eight key codes as bfloat16.
+__device__ __forceinline__ b8 key_values(uint32_t c, float scale)
 {
-    u6 c = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(a, b, scale);
-    asm volatile("" : "+v"(c) : "v"(a), "v"(b), "v"(scale));
-    return c;
-}
-// a, b less what `c` holds of them.
-__device__ __forceinline__ void less_6bit(f16x &a, f16x &b, u6 c, float scale)
-{
-    f32x x = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(c, scale);
-    asm volatile("" : "+v"(x) : "v"(c), "v"(scale));
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        a[i] -= x[2 * i];
-        b[i] -= x[2 * i + 1];
-    }
-}
-__device__ __forceinline__ i8x operand(const u4 &x) { return i8x{(int)x[0], (int)x[1], (int)x[2], (int)x[3], 0, 0, 0, 0}; }
-
-// E2M1 codes times E2M3 ones; SA, SB: the byte of the scales' word.
-template <int SA, int SB>
-__device__ __forceinline__ f4 multiply(const i8x &codes, uint32_t sa, const i8x &part, uint32_t sb, f4 acc)
-{
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(codes, part, acc, 4, 2, SA, (int)sa, SB, (int)sb);
+    struct {
+        b2 v[4];
+    } x = {{__builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((int)c, scale, 0), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((int)c, scale, 1),
+            __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((int)c, scale, 2), __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((int)c, scale, 3)}};
+    return __builtin_bit_cast(b8, x);
 }
 
-// 32 elements of a query row, even and odd ones, and the largest one's bits.
-__device__ __forceinline__ uint32_t query_row(const bf16_t *q, f16x &a, f16x &b)
-{
-    u4 raw[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) raw[i] = fc_load_any<u4>(q + i * 8);
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        a[i] = __uint_as_float(raw[i / 4][i % 4] << 16);
-        b[i] = __uint_as_float(raw[i / 4][i % 4] & 0xffff0000u);
-        top = max(top, max(__float_as_uint(a[i]) & 0x7fffffffu, __float_as_uint(b[i]) & 0x7fffffffu));
-    }
-    return top;
-}
-__device__ __forceinline__ uint32_t query_row(const float *q, f16x &a, f16x &b)
-{
-    f4 raw[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) raw[i] = fc_load_any<f4>(q + i * 4);
-    uint32_t top = 0;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        a[i] = raw[i / 2][i % 2 * 2];
-        b[i] = raw[i / 2][i % 2 * 2 + 1];
-        top = max(top, max(__float_as_uint(a[i]) & 0x7fffffffu, __float_as_uint(b[i]) & 0x7fffffffu));
-    }
-    return top;
-}
-
-// Query rows as operands: N multiplies of a row tile, PARTS of 6 bits.  Heads of 128: a multiply each.  Heads of 64: a part is half a multiply (the
-// lower lanes' keys against an even one, the upper lanes' against the next; the sixth half of three parts is zero).
+// Query rows of a wave as operands: PARTS of bfloat16, N multiplies each.  A lane has the elements that its key codes are multiplied by: those of block
+// lane / 16, or (heads of 64) half a block.
 template <typename T, int DH, int RT>
 struct Queries {
-    static constexpr int PARTS = sizeof(T) == 4 ? 6 : 3, N = DH == 128 ? PARTS : (PARTS + 1) / 2;
-    u4 lo[RT][N][64];
-    u2 hi[RT][N][64];
-    uint32_t scale[RT][(N + 3) / 4][64];
-
-    __device__ __forceinline__ void fill(const T *q, int rt, int lane)  // q: the lane's 32 elements
+    static constexpr int PARTS = sizeof(T) == 4 ? 3 : 1, N = DH / 32;
+    b8 x[RT][PARTS][N];
+    static __device__ __forceinline__ int first(int lane) { return DH == 128 ? lane / 16 * 32 : (lane / 16 & 1) * 32 + lane / 32 * 16; }
+    __device__ __forceinline__ void load(const bf16_t *q, int rt)
     {
-        f16x a, b;
-        const uint32_t top = query_row(q, a, b);
-        // The largest goes to 4 .. 7.5; below 2^-88 nothing need be exact.  At most a quarter of a unit is left: 4 in units of 2^-4, and of
-        // that an eighth: 4 in units of 2^-5.
-        const uint32_t e = max((top >> 23) + ((top & 0x7fffffu) > 0x700000u ? 1 : 0), 40u) - 2;
-        const bool bad = top >= 0x7f800000u;  // not a number, and neither are the scores
-        u6 keep = {};
-        uint32_t word = 0, kept = 0;
 #pragma unroll
-        for (int i = 0; i < PARTS; ++i) {
-            uint32_t s = i ? e + 1 - 5 * i : e;
-            const u6 part = to_6bit(a, b, __uint_as_float(s << 23));
-            if (i + 1 < PARTS) less_6bit(a, b, part, __uint_as_float(s << 23));
-            if (bad) s = 255;
-            int at = i;
-            u6 x = part;
-            if constexpr (DH == 64) {
-                const bool upper = lane >= 32, last = i + 1 == PARTS;
-                if (i % 2 == 0) {
-                    keep = part;
-                    kept = s;
-                    if (!last) continue;
-                }
-                x = upper ? (i % 2 ? part : u6{}) : keep;
-                s = upper ? s : kept;
-                at = i / 2;
-            }
-            lo[rt][at][lane] = u4{x[0], x[1], x[2], x[3]};
-            hi[rt][at][lane] = u2{x[4], x[5]};
-            word |= s << (at % 4 * 8);
-            if (at % 4 == 3 || i + 1 == PARTS) {
-                scale[rt][at / 4][lane] = word;
-                word = 0;
-            }
-        }
+        for (int i = 0; i < N; ++i) x[rt][0][i] = __builtin_bit_cast(b8, fc_load_any<u4>(q + i * 8));
     }
-    __device__ __forceinline__ i8x get(int rt, int i, int lane) const
+    __device__ __forceinline__ void load(const float *q, int rt)
     {
-        const u4 x = lo[rt][i][lane];
-        const u2 y = hi[rt][i][lane];
-        return i8x{(int)x[0], (int)x[1], (int)x[2], (int)x[3], (int)y[0], (int)y[1], 0, 0};
+        struct {
+            f4 v[2 * N];
+        } raw;
+#pragma unroll
+        for (int i = 0; i < 2 * N; ++i) raw.v[i] = fc_load_any<f4>(q + i * 4);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            uint32_t word[PARTS][4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float a = raw.v[2 * i + j / 2][j % 2 * 2], b = raw.v[2 * i + j / 2][j % 2 * 2 + 1];
+#pragma unroll
+                for (int k = 0; k < PARTS; ++k) {  // the upper 16 bits; what they leave is exact, and after three parts nothing
+                    const uint32_t ua = __float_as_uint(a), ub = __float_as_uint(b);
+                    word[k][j] = __builtin_amdgcn_perm(ub, ua, 0x07060302);
+                    a -= __uint_as_float(ua & 0xffff0000u);
+                    b -= __uint_as_float(ub & 0xffff0000u);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < PARTS; ++k) x[rt][k][i] = __builtin_bit_cast(b8, word[k]);
+        }
     }
 };
 
@@ -207,10 +152,9 @@ template <typename T, int DH, int RT, int W>
 __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) void k_q4_attn(AttnArgs p)
 {
     constexpr bool FULL = sizeof(T) == 4;
-    constexpr int DT = DH / 16, N = Queries<T, DH, RT>::N;
-    static_assert(RT <= W, "a wave converts one row tile at most");
+    using Q = Queries<T, DH, RT>;
+    constexpr int DT = DH / 16;
     __shared__ f4 s_o[W][RT][DT][64];
-    __shared__ Queries<T, DH, RT> s_q;
     __shared__ float s_ref[W][RT * 16], s_sum[W][RT * 16];
     __shared__ __align__(16) float s_start[W][64], s_f[W][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -244,19 +188,11 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
         cur.load_keys(rsrc, (uint32_t)t * fc_q4_tile_bytes(DH), lane);
         cur.load_values(rsrc, (uint32_t)t * fc_q4_tile_bytes(DH), lane);
     }
-    if (wave < RT) {
-        const size_t row = min(row0 + wave * 16 + m, p.rows - 1);
-        s_q.fill((const T *)p.q + (((size_t)b * p.Hq + (size_t)j * p.g) * p.A + row) * DH + (DH == 128 ? g : g & 1) * 32, wave, lane);
-    }
-    __syncthreads();
-    i8x q[RT][N];
-    uint32_t qs[RT][(N + 3) / 4];
+    Q q;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-#pragma unroll
-        for (int i = 0; i < (N + 3) / 4; ++i) qs[rt][i] = s_q.scale[rt][i][lane];
-#pragma unroll
-        for (int i = 0; i < N; ++i) q[rt][i] = s_q.get(rt, i, lane);
+        const size_t row = min(row0 + rt * 16 + m, p.rows - 1);
+        q.load((const T *)p.q + (((size_t)b * p.Hq + (size_t)j * p.g) * p.A + row) * DH + Q::first(lane), rt);
     }
     // The next tile's keys are loaded as soon as these are multiplied, its values likewise.  (Always, the last one once more: behind a
     // condition the compiler could not tell them from this tile's and would wait for them.)
@@ -265,8 +201,9 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
         // The row of this lane's scale byte: exponent / c, where the key multiply starts from, and 2^-exponent; then every lane takes those of
         // the sixteen rows whose weights it holds.
         {
-            const float e = (float)max(cur.vs >> (lane % 4 * 8) & 255, (uint32_t)(FC_Q4_V_LOWEST + 127)) - 127.f;  // (a row never stored has 0)
-            float start = FULL ? e : e * p.by_c, f = __builtin_amdgcn_exp2f(-e);
+            const uint32_t byte = cur.vs >> (lane % 4 * 8) & 255;
+            const float e = (float)max(byte, (uint32_t)(FC_Q4_V_LOWEST + 127)) - 127.f;  // (a row never stored has 0)
+            float start = byte == 255 ? __builtin_nanf("") : FULL ? e : e * p.by_c, f = __builtin_amdgcn_exp2f(-e);
             if ((t + 1) * 64 > n) {  // rows behind the end may hold anything: weight 0, and key scales that leave scores finite
                 if (t * 64 + lane % 16 / 4 * 16 + g * 4 + lane % 4 >= n) {
                     start = -__builtin_inff();
@@ -286,19 +223,22 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
         f4 s[RT][4];
         bool move = false;
         float top[RT];
-// (part by part: products that add to one another are a latency of the matrix core apart; the least first, so that they are not rounded to the
-// largest)
-#define FC_Q4_KEYS(K, I)                                                                    \
-    _Pragma("unroll") for (int rt = 0; rt < RT; ++rt) s[rt][K] =                              \
-        multiply<K, I % 4>(operand(cur.k[K]), cur.ks, q[rt][I], qs[rt][I / 4], I != FIRST ? s[rt][K] : FULL ? f4{0.f, 0.f, 0.f, 0.f} : start[K]);
-#define FC_Q4_PART(I) FC_Q4_KEYS(0, I) FC_Q4_KEYS(1, I) FC_Q4_KEYS(2, I) FC_Q4_KEYS(3, I)
-        constexpr int FIRST = N - 1;
-        if constexpr (N == 6) { FC_Q4_PART(5) FC_Q4_PART(4) FC_Q4_PART(3) }
-        if constexpr (N >= 3) { FC_Q4_PART(2) }
-        FC_Q4_PART(1)
-        FC_Q4_PART(0)
-#undef FC_Q4_PART
-#undef FC_Q4_KEYS
+        // (the least part first; products that add to one another are a latency of the matrix core apart)
+#pragma unroll
+        for (int i = 0; i < Q::N; ++i) {
+            b8 keys[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) keys[k] = key_values(cur.k[k][i], __uint_as_float((cur.ks >> (8 * k) & 255) << 23));
+#pragma unroll
+            for (int part = Q::PARTS - 1; part >= 0; --part)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) {
+                        const f4 sum = i || part + 1 < Q::PARTS ? s[rt][k] : FULL ? f4{0.f, 0.f, 0.f, 0.f} : start[k];
+                        s[rt][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(keys[k], q.x[rt][part][i], sum, 0, 0, 0);
+                    }
+        }
         cur.load_keys(rsrc, next, lane);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
