@@ -273,7 +273,9 @@ fc_status fc_q4_read_rows(const fc_q4_cache *cache, int32_t layer, void *k_rows,
 size_t fc_q4_workspace_bytes(const fc_config *cfg, int32_t max_rows);
 
 /* Bidirectional attention of the window's queries over rows [0, kv_len), or over [0, min(kv_lens[b], kv_len)) of sequence b:
- * as fc_active_attention, with the values that the rows stand for.
+ * as fc_active_attention, with the values that the rows stand for.  Scores, weights and their sum are held in fp32.  What the values are multiplied by, a
+ * row's weight times the power of two of its value row, is rounded to fp16 (bf16 caches): 2^-11 of itself down to 2^-21 of the
+ * largest such product, half of 2^-31 of the largest below that.  fp32 caches: to 2^-21 of itself, 2^-43 of the largest.
  *   q        device [B][Hq][A][Dh]
  *   kv_lens  device int32 [B] or NULL; a sequence of length 0 (or less) has zeros in out
  *   pos      device int32 [B][A] or NULL; rows with a negative entry produce zeros

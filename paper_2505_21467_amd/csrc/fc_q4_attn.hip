@@ -11,9 +11,10 @@
 //    the result, and four take as long as the conversions.  As two 8-bit numbers its products would be cut off at 2^-14 of their sum.)
 //  - Weights.  Value row t is codes times 2^e_t.  The power goes into the exponent of the row's weight, w_t = 2^(s_t + e_t - r), so the codes
 //    are multiplied as they are, and the sum that divides adds w_t 2^-e_t.  The key multiply starts from e_t over the softmax scale, so this
-//    costs nothing.  The reference r only has to keep w_t in range: it moves when a score passes it by 2^MOVE, which after the first
-//    tiles is rare.  Weights are rounded to fp16 (11 bits; bfloat16 would add as much error as rounding the output does, two E2M3 parts
-//    more, 2.8e-3 for 1.7e-3 relative in all), sums are fp32.
+//    costs nothing.  The reference r only has to keep w_t in range: it is set 2^7 below the largest and moves when a score passes it by 2^15, which after
+//    the first tiles is rare.  Weights are rounded to fp16: 11 bits down to 2^-21 of the largest, none below 2^-32 (half a step of the least
+//    number; the sum that divides has them all, in fp32).  bfloat16 would add as much error as rounding the output does, two E2M3 parts
+//    more, 2.8e-3 for 1.7e-3 relative in all.  Sums are fp32.
 //  - fp32 rows are three bfloat16 numbers, 8 bits each, which is all of them, and a weight is two fp16 numbers, the second in units of 2^-12 with sums
 //    of its own: 2^-23 of the weight.  The reference is a whole number and e_t - r is added with the scale, so a score is rounded once.
 //    Errors against 64 bits are 1.6e-7 (heads of 64) and 2.2e-7 (128), less than half of a plain fp32 computation's; 32 rows x 28 heads over
@@ -39,7 +40,8 @@ typedef __bf16 b2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
-constexpr float MOVE = 8.f;  // a score may pass the reference by 2^MOVE
+constexpr float LIFT = 7.f;   // a row's largest weight so far is 2^LIFT when its reference is set
+constexpr float MOVE = 15.f;  // and none may pass 2^MOVE: fp16 ends at 65504
 constexpr float FINE = 4096.f;  // fp32: what a weight's fp16 lacks is multiplied in units of 1 / FINE
 template <typename T> constexpr int MOST_RT = sizeof(T) == 4 ? 1 : 2;  // row tiles of a workgroup
 
@@ -258,7 +260,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
                 float x = top[rt];
                 x = fmaxf(x, __shfl_xor(x, 16));
                 x = fmaxf(x, __shfl_xor(x, 32));
-                const float r = fmaxf(ref[rt], FULL ? ceilf(x) : x), a = __builtin_amdgcn_exp2f(ref[rt] - r);
+                const float r = fmaxf(ref[rt], (FULL ? ceilf(x) : x) - LIFT), a = __builtin_amdgcn_exp2f(ref[rt] - r);
                 ref[rt] = r;
                 sum[rt] *= a;
 #pragma unroll
