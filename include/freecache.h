@@ -424,7 +424,7 @@ fc_status fc_gather_rows(int32_t dtype, const void *table, int32_t rows, int32_t
  *   tok[m] = the first entry of the order at which the running sum of w exceeds u[m] W,   conf[m] = w[tok[m]] / W.
  * temperature 0 is the arg-max with conf = softmax(z)[tok] as in fc_lm_head_argmax; top_k, top_p, min_p and u are then not looked at.
  * A row gives the same bits from call to call and whatever else is in the batch.  Weights are exact to 2^-33 of themselves; entries 32 temperatures and more
- * below the largest (w < 1.3e-14) count as w = 0.  NaN entries are passed over, -inf ones have w = 0; of several +inf each has w = 1 and
+ * below the largest (w < 1.3e-14; some from 31.96 on) count as w = 0 and are not kept.  NaN entries are passed over, -inf ones have w = 0; of several +inf each has w = 1 and
  * the finite ones 0.  A row of nothing but NaN and -inf gets tok = -1, conf = 0 (fc_unmask_select would write that -1: it is the caller's to
  * look for).
  */
@@ -433,7 +433,7 @@ fc_status fc_gather_rows(int32_t dtype, const void *table, int32_t rows, int32_t
 size_t fc_sample_workspace_bytes(int32_t dtype, int32_t M, int32_t V);
 
 /*   logits  device [M][ld] (element type dtype), of which the first V entries of a row count; ld >= V elements, any alignment of elements
- *   u       device float [M], uniform in [0, 1); below 0 counts as 0, 1 or more (and NaN) picks the last kept entry.  May be NULL at temperature 0.
+ *   u       device float [M], uniform in [0, 1); below 0 counts as 0, 1 or more (and NaN) picks the last kept entry, whatever its weight.  May be NULL at temperature 0.
  *   tok  device int32 [M];  conf  device float [M];  workspace  device, 16-byte aligned, >= fc_sample_workspace_bytes(dtype, M, V) bytes
  * Errors: INVALID_ARG (NULL; M, V < 1; ld < V; temperature < 0 or not finite; top_k < 0; top_p outside (0, 1]; min_p outside [0, 1]),
  * UNSUPPORTED (V beyond 2^24, M beyond 65535, M * V beyond 2^36), WORKSPACE, HIP.  Two calls that overlap in time must not share a workspace. */

@@ -359,11 +359,12 @@ struct PickShared {
     Entry few[FEW];
     Aim aim;
     unsigned long long ones, zeros, shared, sum_found, rank_found, weight_found;
-    uint32_t n, digit, count_found;
+    uint32_t n, digit, count_found, upto_found;
 };
 
 struct Found {
     uint64_t rank, sum, weight;  // the entry, the weight of all up to it, its own
+    uint32_t count;              // the number of all up to it
 };
 
 // Of n entries, one a lane: number and weight of those before this lane's.
@@ -492,10 +493,11 @@ __device__ Found select(PickShared &s, bool counting, uint32_t n, uint64_t targe
             s.rank_found = own.rank;
             s.sum_found = run + own.weight;
             s.weight_found = own.weight;
+            s.upto_found = count + runs + 1;
         }
     }
     __syncthreads();
-    return Found{s.rank_found, s.sum_found, s.weight_found};
+    return Found{s.rank_found, s.sum_found, s.weight_found, s.upto_found};
 }
 
 // What select() finds, in one wave without a barrier: entries of bin b in the list, FEW at most.
@@ -526,7 +528,8 @@ __device__ __attribute__((noinline)) Found select_few(PickShared &s, bool counti
     const bool passes = counting ? runs + 1 > target : to > target, before = counting ? runs > target : run > target;
     const uint64_t mask = __ballot((uint32_t)lane < n && ((passes && !before) || (!passes && runs == n - 1)));
     const int at = mask ? __builtin_ctzll(mask) : 0;
-    return Found{(uint64_t)__shfl((unsigned long long)own.rank, at), (uint64_t)__shfl((unsigned long long)to, at), (uint64_t)__shfl((unsigned long long)own.weight, at)};
+    return Found{(uint64_t)__shfl((unsigned long long)own.rank, at), (uint64_t)__shfl((unsigned long long)to, at), (uint64_t)__shfl((unsigned long long)own.weight, at),
+                 (uint32_t)__shfl((int)runs, at) + 1};
 }
 
 // The entries of bin b in the list, PICK at most: one a thread.
@@ -706,11 +709,14 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
     auto reach = [&](double x, bool past) { return search([&](int b) { return past ? s.cum[b] > x : s.cum[b] >= x; }); };
     const double all = s.cum[BINS - 1], u = p.greedy ? 0. : (double)p.u[row];
     const bool inside = u < 1.;  // (NaN: not)
-    // The bin of the token for this total of kept weights: where u times it is exceeded, or the last kept entry's.
-    auto token_bin = [&](double total) {
-        const int b = inside ? reach(fmax(u, 0.) * total, true) : reach(total, false);
-        return b < BINS ? b : reach(all, false);
+    // The last bin up to b that has entries (the first has).  Running sums are rounded, by lanes in their own order, so that one may exceed another
+    // behind an empty bin.
+    auto occupied = [&](int b) {
+        const uint32_t n = s.count[b];
+        return n > counted(b) ? b : search([&](int b) { return s.count[b] >= n; });
     };
+    // The bin of the token for this total of kept weights: where u times it is exceeded.
+    auto token_bin = [&](double total) { return occupied(min(reach(fmax(u, 0.) * total, true), BINS - 1)); };
 
     // Where the targets can lie: the total is known but for the bins in which filters end.  One wave finds out, while the others leave it the compute
     // unit.
@@ -723,8 +729,8 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
             high = s.cum[kb];
         }
         if (p.top_p < 1.f) {
-            pb0 = min(reach((double)p.top_p * low, false), BINS - 1);
-            pb1 = kb < BINS ? min(reach((double)p.top_p * high, false), BINS - 1) : pb0;
+            pb0 = occupied(min(reach((double)p.top_p * low, false), BINS - 1));
+            pb1 = kb < BINS ? occupied(min(reach((double)p.top_p * high, false), BINS - 1)) : pb0;
             low = fmin(low, before(pb0));
             high = fmin(high, s.cum[pb1]);
         }
@@ -743,7 +749,16 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
             pb1 = -1;
         }
         if (pb1 < 0 && mb < kb) kb = BINS;
-        const int sb0 = token_bin(low), sb1 = low < high ? token_bin(high) : sb0;
+        int sb0, sb1;
+        if (inside) {
+            sb0 = token_bin(low);
+            sb1 = low < high ? token_bin(high) : sb0;
+        } else {  // the last kept entry: in the first bin in which a filter ends, or, if none of a min-p's bin is kept, in the one before
+            sb0 = min(min(kb, mb), pb0);
+            sb1 = min(min(kb, mb), pb1 < 0 ? BINS : pb1);
+            if (sb1 == BINS) sb0 = sb1 = occupied(BINS - 1);
+            else if (sb0 == mb && mb > 0) sb0 = occupied(mb - 1);
+        }
         // Logits of the bin in which top-k ends, of those in which the other filters can, and of the token's.  Where they lie apart with many entries
         // between them, three ranges; else one.
         const int f0 = min(pb0, mb), f1 = max(mb < BINS ? mb : -1, pb1), first = min(min(f0, kb), sb0), final = max(max(f1, kb < BINS ? kb : -1), sb1);
@@ -848,23 +863,30 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
     };
 
     double total = all;
+    uint32_t kept_entries = s.count[BINS - 1];
     if (kb < BINS) {
+        kept_entries = (uint32_t)p.top_k;
         const Found f = pick(true, kb, (uint64_t)p.top_k - counted(kb) - 1);
         total = before(kb) + s.factor[kb] * (double)f.sum;
     }
     if (pb1 >= 0) {
         const double x = (double)p.top_p * total;
-        const int b = min(max(reach(x, false), pb0), pb1);
+        const int b = min(max(occupied(min(reach(x, false), BINS - 1)), pb0), pb1);
         const double y = ceil((x - before(b)) / s.factor[b]) - 1.;  // a sum that reaches x passes the whole number below it
         const Found f = pick(false, b, (uint64_t)fmax(y, 0.));
         total = fmin(total, before(b) + s.factor[b] * (double)f.sum);
+        kept_entries = min(kept_entries, counted(b) + f.count);
     }
     if (mb < BINS) {  // the last entry that is large enough
         uint64_t kept = 0;
+        uint32_t n = 0;
         const float mlow = g.lowest(mb), mhigh = g.highest(mb);
         auto look = [&](float x) {
             double within;
-            if (x >= mlow && x <= mhigh && g.bin(x, within) == mb && ((double)x - (double)z_max) * p.inv_t >= p.log_min_p) kept += g.weight(within);
+            if (x >= mlow && x <= mhigh && g.bin(x, within) == mb && ((double)x - (double)z_max) * p.inv_t >= p.log_min_p) {
+                kept += g.weight(within);
+                ++n;
+            }
         };
         if (list) {
 #pragma unroll 1
@@ -873,15 +895,23 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
             each_entry<T, PICK>(z, p.V, [&](int, float x) { look(x); });
         }
         sync();
-        if (tid == 0) s.sum_found = 0;
+        if (tid == 0) {
+            s.sum_found = 0;
+            s.upto_found = 0;
+        }
         sync();
-        if (kept) atomicAdd(&s.sum_found, (unsigned long long)kept);
+        if (n) {
+            atomicAdd(&s.sum_found, (unsigned long long)kept);
+            atomicAdd(&s.upto_found, n);
+        }
         sync();
         total = fmin(total, before(mb) + s.factor[mb] * (double)s.sum_found);
+        kept_entries = min(kept_entries, counted(mb) + s.upto_found);
     }
-    const int b = min(max(token_bin(total), sb0), sb1);
-    const double x = ((inside ? fmax(u, 0.) * total : total) - before(b)) / s.factor[b];
-    const Found f = pick(false, b, (uint64_t)fmax(inside ? x : rint(x) - 1., 0.));
+    // (The last kept entry is found by its number: beside the sum its weight may be nothing.)
+    const int b = min(max(inside ? token_bin(total) : search([&](int b) { return s.count[b] >= kept_entries; }), sb0), sb1);
+    const double x = (fmax(u, 0.) * total - before(b)) / s.factor[b];
+    const Found f = pick(!inside, b, inside ? (uint64_t)fmax(x, 0.) : kept_entries - counted(b) - 1);
     if (tid == 0) {
         p.tok[row] = (int32_t)~(uint32_t)f.rank;
         p.conf[row] = (float)((double)f.weight * s.factor[b] / total);
