@@ -423,10 +423,11 @@ fc_status fc_gather_rows(int32_t dtype, const void *table, int32_t rows, int32_t
  * and with W the sum of w over the shortest of the prefixes
  *   tok[m] = the first entry of the order at which the running sum of w exceeds u[m] W,   conf[m] = w[tok[m]] / W.
  * temperature 0 is the arg-max with conf = softmax(z)[tok] as in fc_lm_head_argmax; top_k, top_p, min_p and u are then not looked at.
- * A row gives the same bits from call to call and whatever else is in the batch.  Weights are exact to 2^-33 of themselves; entries 32 temperatures and more
- * below the largest (w < 1.3e-14; some from 31.96 on) count as w = 0 and are not kept.  NaN entries are passed over, -inf ones have w = 0; of several +inf each has w = 1 and
- * the finite ones 0.  A row of nothing but NaN and -inf gets tok = -1, conf = 0 (fc_unmask_select would write that -1: it is the caller's to
- * look for).
+ * A row gives the same bits from call to call and whatever else is in the batch.  Weights are exact to 2^-32 of themselves and, bins
+ * being places of z / temperature, to |z| / temperature times 2^-53 (logits 2^20 temperatures from zero: 2^-33).  Entries 32
+ * temperatures and more below the largest (w < 1.3e-14; some from 31.96 on) count as w = 0 and are not kept.  NaN entries are
+ * passed over, -inf ones have w = 0; of several +inf each has w = 1 and the finite ones 0.  A row of nothing but NaN and -inf gets
+ * tok = -1, conf = 0 (fc_unmask_select would write that -1: it is the caller's to look for).
  */
 
 /* Workspace bytes of fc_sample_tokens for this shape; 0 on bad arguments. */

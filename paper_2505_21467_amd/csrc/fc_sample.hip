@@ -12,8 +12,8 @@
 //     long) from the row, and the targets are found among them by digits of their bits.
 //
 // Whole sums do not depend on the order in which they are made, so a row gives the same bits whatever else is in the batch and however it is
-// cut.  Weights are exact to 2^-33 and their bins' factors to 2^-50: with sums in fp32, undecided rows would get another token once in a
-// hundred.
+// cut.  Weights are exact to 2^-32 and their bins' factors to 2^-50 (and to the rounding of 32 z / T, which matters from |z| / T = 2^20 on): with
+// sums in fp32, undecided rows would get another token once in a hundred.
 #include <math.h>
 
 #include "fc_device.h"
