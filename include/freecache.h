@@ -282,7 +282,7 @@ size_t fc_q4_workspace_bytes(const fc_config *cfg, int32_t max_rows);
  *   out      device [B][A][Hq*Dh]
  *   workspace  device, 16-byte aligned, may be NULL.  Two calls that overlap in time must not share one.
  * Rows behind a sequence's length are not looked at: whatever they hold does not matter.
- * Errors: INVALID_ARG, BOUNDS (layer; kv_len < 1 or > max_seq), UNSUPPORTED (batch * A beyond 2^24; beyond 2^23 row tiles: (batch * n_kv_heads +
+ * Errors: INVALID_ARG, BOUNDS (layer; kv_len < 1 or > max_seq), UNSUPPORTED (batch * A beyond 2^24; 2^23 row tiles or more: (batch * n_kv_heads +
  * 7) times the 16-row tiles of A rows of a kv head's query heads), HIP. */
 fc_status fc_q4_attention(const fc_q4_cache *cache, int32_t layer, const void *q, int32_t A, int32_t kv_len, const int32_t *kv_lens,
                           const int32_t *pos, void *out, void *workspace, size_t workspace_bytes, void *stream);

@@ -1562,9 +1562,9 @@ fc_status fc_q4_attention(const fc_q4_cache *cache, int32_t layer, const void *q
     if (A < 1) return fail(FC_ERR_INVALID_ARG, "A %d must be >= 1", A);
     const fc_config &c = cache->cfg;
     if ((int64_t)A * c.batch > (1 << 24)) return fail(FC_ERR_UNSUPPORTED, "batch * A exceeds 2^24 rows");
-    // (workgroups of up to 512 threads, of which a grid holds 2^32)
-    if (((int64_t)c.batch * c.n_kv_heads + 7) * (((int64_t)A * (c.n_q_heads / c.n_kv_heads) + 15) / 16) > (1 << 23))
-        return fail(FC_ERR_UNSUPPORTED, "more than 2^23 row tiles of 16 rows");
+    // (workgroups of up to 512 threads, of which a grid holds fewer than 2^32)
+    if (((int64_t)c.batch * c.n_kv_heads + 7) * (((int64_t)A * (c.n_q_heads / c.n_kv_heads) + 15) / 16) >= (1 << 23))
+        return fail(FC_ERR_UNSUPPORTED, "2^23 row tiles of 16 rows or more");
     if (kv_len < 1 || kv_len > cache->cfg.max_seq)
         return fail(FC_ERR_BOUNDS, "kv_len %d outside [1, %d]", kv_len, cache->cfg.max_seq);
     if ((uintptr_t)workspace & 15) return fail(FC_ERR_INVALID_ARG, "workspace must be 16-byte aligned");

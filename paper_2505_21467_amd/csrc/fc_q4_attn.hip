@@ -482,7 +482,8 @@ FcQ4Plan plan(const FcQ4Geom &G, int A, int kv_len, size_t cap)
         best.waves = k.q4_waves == 8 || (best.rt == 1 && (k.q4_waves == 1 || k.q4_waves == 2)) ? k.q4_waves : 4;
         best.splits = k.q4_splits > 0 ? k.q4_splits : 1;
         if (best.splits > tiles) best.splits = (int)tiles;
-        while (best.splits > 1 && fc_q4_plan_workspace(G, best, A) > cap) --best.splits;
+        const int64_t groups = (rows + 16 * best.rt - 1) / (16 * best.rt);
+        while (best.splits > 1 && (fc_q4_plan_workspace(G, best, A) > cap || (pairs * best.splits + 7) * groups >= 1 << 23)) --best.splits;
         return best;
     }
     double least = 1e30;
