@@ -430,7 +430,7 @@ fc_status fc_gather_rows(int32_t dtype, const void *table, int32_t rows, int32_t
  * tok = -1, conf = 0 (fc_unmask_select would write that -1: it is the caller's to look for).
  */
 
-/* Workspace bytes of fc_sample_tokens for this shape; 0 on bad arguments. */
+/* Workspace bytes of fc_sample_tokens for this shape; 0 for one that the call refuses. */
 size_t fc_sample_workspace_bytes(int32_t dtype, int32_t M, int32_t V);
 
 /*   logits  device [M][ld] (element type dtype), of which the first V entries of a row count; ld >= V elements, any alignment of elements

@@ -1579,7 +1579,7 @@ fc_status fc_q4_attention(const fc_q4_cache *cache, int32_t layer, const void *q
 
 size_t fc_sample_workspace_bytes(int32_t dtype, int32_t M, int32_t V)
 {
-    if ((dtype != FC_F32 && dtype != FC_BF16) || M < 1 || V < 1 || M > 65535 || V > (1 << 24)) return 0;
+    if ((dtype != FC_F32 && dtype != FC_BF16) || M < 1 || V < 1 || M > 65535 || V > (1 << 24) || (int64_t)M * V > ((int64_t)1 << 36)) return 0;
     return fc_sample_workspace(dtype, M, V);
 }
 

@@ -13,3 +13,10 @@ def test_row_tiles_whose_threads_do_not_fit_a_grid():
         h = fc.fc_q4_alloc(cfg, FAKE)
         _raises(fc.FC_ERR_UNSUPPORTED, A, h, 0, FAKE, rows, 100, None, None, FAKE, FAKE, 1 << 30, 0)
         fc.fc_q4_free(h)
+
+
+def test_workspace_of_logits_beyond_what_a_call_takes():
+    """0 wherever the call refuses the shape."""
+    W = fc.fc_sample_workspace_bytes
+    assert W("bf16", 65535, 1 << 21) == 0 and W("f32", 4097, 1 << 24) == 0
+    assert W("bf16", 4096, 1 << 24) > 0 and W("f32", 32768, 1 << 21) > 0        # 2^36 itself
