@@ -242,7 +242,7 @@ size_t fc_q4_storage_bytes(const fc_config *cfg);
 
 /* Create a handle.  storage: device buffer of fc_q4_storage_bytes() bytes, 16-byte aligned, borrowed for the life of the handle, or NULL to
  * let the library allocate zero-filled storage that it then owns.  Zeroed storage reads as zeros.  Nothing else is allocated.
- * Errors: INVALID_ARG, UNSUPPORTED (geometry; more than 65535 batch * n_kv_heads), OOM. */
+ * Errors: INVALID_ARG, UNSUPPORTED (geometry; more than 65535 batch * n_kv_heads; a softmax_scale outside [2^-100, 2^100]), OOM. */
 fc_status fc_q4_alloc(const fc_config *cfg, void *storage, fc_q4_cache **out);
 
 /* Destroy the handle and free library-owned storage.  The caller must have synchronised every stream that used it.  NULL is accepted. */

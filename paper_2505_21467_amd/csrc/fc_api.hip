@@ -1421,6 +1421,9 @@ fc_status check_q4_config(const fc_config *c)
     fc_status st = check_config(c);
     if (st != FC_OK) return st;
     if ((int64_t)c->batch * c->n_kv_heads > 65535) return fail(FC_ERR_UNSUPPORTED, "batch * n_kv_heads is limited to 65535");
+    // (the attention's scores start from a value row's power over the scale)
+    if (c->softmax_scale > 0.f && !(c->softmax_scale >= 0x1p-100f && c->softmax_scale <= 0x1p100f))
+        return fail(FC_ERR_UNSUPPORTED, "softmax_scale %g outside [2^-100, 2^100]", (double)c->softmax_scale);
     return FC_OK;
 }
 

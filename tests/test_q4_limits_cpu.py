@@ -20,3 +20,12 @@ def test_workspace_of_logits_beyond_what_a_call_takes():
     W = fc.fc_sample_workspace_bytes
     assert W("bf16", 65535, 1 << 21) == 0 and W("f32", 4097, 1 << 24) == 0
     assert W("bf16", 4096, 1 << 24) > 0 and W("f32", 32768, 1 << 21) > 0        # 2^36 itself
+
+
+def test_softmax_scales_whose_inverse_no_float_holds():
+    """The scores start from the value rows' powers over the scale: from 2^-100 to 2^100, and the default."""
+    for scale in (1e-38, 1e-44, 2.0 ** -101, 2.0 ** 101, 3e38):
+        _raises(fc.FC_ERR_UNSUPPORTED, fc.fc_q4_alloc, _cfg(softmax_scale=scale), FAKE)
+        assert fc.fc_q4_storage_bytes(_cfg(softmax_scale=scale)) == 0 and fc.fc_q4_workspace_bytes(_cfg(softmax_scale=scale), 4) == 0
+    for scale in (0.0, 2.0 ** -100, 2.0 ** 100, 0.125):
+        fc.fc_q4_free(fc.fc_q4_alloc(_cfg(softmax_scale=scale), FAKE))
