@@ -374,7 +374,6 @@ __device__ __forceinline__ uint64_t of_lane(uint64_t x, uint32_t lane)
 }
 __device__ __forceinline__ void before_own(const Entry &own, uint32_t n, uint64_t &weight, uint32_t &count)
 {
-#pragma unroll 4
     for (uint32_t i = 0; i < n; ++i) {
         const uint64_t rank = of_lane(own.rank, i), w = of_lane(own.weight, i);
         weight += rank > own.rank ? w : 0;
@@ -614,7 +613,8 @@ __device__ __forceinline__ void fetch(PickShared &s, const T *z, int from, int t
     }
 }
 
-// Those of one range.  (Apart from the kernel, since it is rare; what is not is in it, as a call saves registers in memory.)
+// Those of one range.  (Apart from the kernel, since it is rare.  What every row runs keeps its registers over the calls in it; only select_in() over
+// the row itself saves some in memory.)
 template <typename T>
 __device__ __attribute__((noinline)) void fetch_range(PickShared &s, const T *z, int V, float least, float most)
 {
