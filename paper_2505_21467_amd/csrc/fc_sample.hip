@@ -206,7 +206,7 @@ __global__ __launch_bounds__(SCAN) void k_sample_bins(FcSampleArgs p, int parts,
 {
     constexpr int N = Piece<T>::N, PIECES = PART / (SCAN * N);
     __shared__ unsigned long long s_bin[BINS];
-    __shared__ uint32_t s_count[BINS], s_wave[SCAN / 64], s_n, s_pieces;
+    __shared__ uint32_t s_count[BINS], s_wave[SCAN / 64], s_n, s_pieces[2];
     __shared__ float s_max[SCAN / 64];
     __shared__ int s_last[2];
     __shared__ uint16_t s_piece[PIECES * SCAN];
@@ -237,7 +237,7 @@ __global__ __launch_bounds__(SCAN) void k_sample_bins(FcSampleArgs p, int parts,
     }
     if (tid == 0) {
         s_last[0] = s_last[1] = BINS;
-        s_n = s_pieces = 0;
+        s_n = s_pieces[0] = s_pieces[1] = 0;
     }
     __syncthreads();
 #pragma unroll
@@ -270,26 +270,23 @@ __global__ __launch_bounds__(SCAN) void k_sample_bins(FcSampleArgs p, int parts,
         // wave has some.  Those with an entry for the list come first, the others from behind, so that most waves need not ask for places in it.
         const float first_cut = g.lowest(end);
         const bool some_others = __builtin_amdgcn_readfirstlane(end < last);  // (under a small top-k all that matters is listed)
+        auto note = [&](uint32_t &number, auto wanted, auto place) {
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
-            const bool first = best[i] >= first_cut;
-            const uint64_t firsts = __ballot(first);
-            bool other = false;
-            uint64_t others = 0;
-            if (some_others) {
-                other = !first && best[i] >= cut;
-                others = __ballot(other);
+            for (int i = 0; i < PIECES; ++i) {
+                const bool mine = wanted(best[i]);
+                const uint64_t in = __ballot(mine);
+                if (!in) continue;
+                uint32_t base = 0;
+                if (tid % 64 == 0) base = atomicAdd(&number, (uint32_t)__builtin_popcountll(in));
+                base = __builtin_amdgcn_readfirstlane(base);
+                const uint32_t to = __builtin_amdgcn_mbcnt_hi((uint32_t)(in >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in, base));
+                if (mine) s_piece[place(to)] = (uint16_t)(i * SCAN + tid);
             }
-            if (!(firsts | others)) continue;
-            uint32_t base = 0;
-            if (tid % 64 == 0) base = atomicAdd(&s_pieces, (uint32_t)__builtin_popcountll(others) << 16 | (uint32_t)__builtin_popcountll(firsts));
-            base = __builtin_amdgcn_readfirstlane(base);
-            const uint64_t mine = first ? firsts : others;
-            const uint32_t to = __builtin_amdgcn_mbcnt_hi((uint32_t)(mine >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mine, first ? base & 0xffff : base >> 16));
-            if (first || other) s_piece[first ? to : PIECES * SCAN - 1 - to] = (uint16_t)(i * SCAN + tid);
-        }
+        };
+        note(s_pieces[0], [&](float x) { return x >= first_cut; }, [](uint32_t to) { return to; });
+        if (some_others) note(s_pieces[1], [&](float x) { return x >= cut && !(x >= first_cut); }, [](uint32_t to) { return PIECES * SCAN - 1 - to; });
         __syncthreads();
-        const int firsts = (int)(s_pieces & 0xffff), pieces = firsts + (int)(s_pieces >> 16);
+        const int firsts = (int)s_pieces[0], pieces = firsts + (int)s_pieces[1];
 #pragma unroll 1
         for (int i = tid; i < pieces; i += SCAN) {
             const int first = from + s_piece[i < firsts ? i : PIECES * SCAN - 1 - (i - firsts)] * N;
