@@ -438,24 +438,34 @@ struct Q4Shape {
     int rt, waves;
     double start, wave, unit, wg, merge, range, mb, part;
 };
-const Q4Shape Q4_128[] = {{1, 1, 4.84, 0.614, 0.173, 0.34, 1.81, 0.072, 0.387, 0.50},
-                          {1, 2, 4.31, 0.638, 0.174, 0.45, 2.14, 0.075, 0.299, 1.0},
-                          {1, 4, 4.10, 0.642, 0.149, 0.79, 2.18, 0.074, 0.318, 0.46},
-                          {1, 8, 3.50, 1.049, 0.157, 2.24, 2.01, 0.073, 0.373, 0.66},
-                          {2, 4, 4.89, 0.914, 0.237, 1.52, 2.14, 0.084, 0.303, 0.59},
-                          {2, 8, 4.10, 1.596, 0.243, 2.84, 2.00, 0.081, 0.408, 1.0}};
-const Q4Shape Q4_64[] = {{1, 1, 4.07, 0.460, 0.117, 0.25, 1.91, 0.079, 0.461, 0.35},
-                         {1, 2, 3.81, 0.482, 0.107, 0.33, 2.08, 0.082, 0.398, 0.89},
-                         {1, 4, 3.70, 0.490, 0.090, 0.44, 2.18, 0.079, 0.353, 0.66},
-                         {1, 8, 3.53, 0.773, 0.085, 1.11, 2.19, 0.068, 0.329, 0.51},
-                         {2, 4, 4.29, 0.708, 0.137, 0.68, 2.23, 0.070, 0.469, 1.0},
-                         {2, 8, 3.64, 1.154, 0.154, 2.04, 2.36, 0.046, 0.657, 0.76}};
+const Q4Shape Q4_128[] = {{1, 1, 3.85, 0.716, 0.193, 0.29, 1.71, 0.079, 0.353, 0.98},
+                          {1, 2, 3.25, 0.766, 0.217, 0.39, 2.07, 0.081, 0.367, 1.00},
+                          {1, 4, 3.06, 0.777, 0.175, 0.69, 2.19, 0.079, 0.345, 0.68},
+                          {1, 8, 2.47, 1.270, 0.195, 1.79, 2.21, 0.083, 0.295, 0.72},
+                          {2, 4, 3.93, 1.096, 0.275, 1.43, 2.29, 0.063, 0.331, 0.56},
+                          {2, 8, 3.11, 1.933, 0.331, 2.82, 2.39, 0.052, 0.320, 0.60}};
+const Q4Shape Q4_64[] = {{1, 1, 3.09, 0.557, 0.134, 0.12, 1.83, 0.073, 0.554, 1.00},
+                         {1, 2, 2.85, 0.603, 0.117, 0.22, 2.02, 0.070, 0.633, 1.00},
+                         {1, 4, 2.76, 0.599, 0.107, 0.31, 2.09, 0.067, 0.515, 1.00},
+                         {1, 8, 2.70, 0.868, 0.107, 0.72, 2.06, 0.059, 0.452, 0.66},
+                         {2, 4, 3.40, 0.829, 0.173, 0.64, 2.02, 0.054, 0.573, 0.70},
+                         {2, 8, 2.72, 1.348, 0.213, 1.51, 2.04, 0.036, 0.694, 0.92}};
+const Q4Shape Q4_F32_128[] = {{1, 1, 4.35, 1.166, 0.306, 0.55, 1.83, 0.087, 0.311, 0.06},
+                              {1, 2, 3.91, 1.179, 0.474, 0.56, 2.18, 0.094, 0.215, 1.00},
+                              {1, 4, 3.68, 1.244, 0.363, 1.22, 2.26, 0.090, 0.247, 0.40},
+                              {1, 8, 2.61, 2.277, 0.489, 2.31, 2.27, 0.086, 0.297, 0.62}};
+const Q4Shape Q4_F32_64[] = {{1, 1, 3.43, 0.801, 0.226, 0.20, 2.13, 0.059, 0.362, 0.22},
+                             {1, 2, 3.30, 0.805, 0.316, 0.09, 2.24, 0.076, 0.269, 1.00},
+                             {1, 4, 3.13, 0.819, 0.229, 0.38, 2.38, 0.044, 0.419, 0.60},
+                             {1, 8, 2.93, 1.347, 0.274, 1.25, 2.29, 0.000, 0.754, 0.59}};
 
 // Estimated time of a call: the longest of a wave's chain of tiles, a compute unit's tiles and the stream from HBM, joined by a 4-norm, and the rest.
-// The load of a compute unit is that of the die with the most units.  Fitted to 4068 measured (shape, plan) pairs of 160 shapes (1 .. 8 sequences, 1 ..
-// 32 kv heads, 1 .. 8 query heads each, 1 .. 256 rows, 8 .. 16800 keys from HBM; rms error 4 .. 9 %); the plan it picks is 1.4 %
-// slower than the best measured one in the mean, 14 % at most.  One wave and two are for few keys and many rows: 4 sequences, 8 kv heads of 7, 160
-// rows, 32 keys take 10.1 us with one, 14.5 with four; 8 sequences, 28 / 4 heads, 256 rows, 128 keys 16.5 and 23.2.
+// The load of a compute unit is that of the die with the most units.  Fitted to 3804 measured (shape, plan) pairs of 160 shapes in bf16 and 1744 of 80 in
+// fp32 (1 .. 8 sequences, 1 .. 32 kv heads, 1 .. 8 query heads each, 1 .. 256 rows, 8 .. 16800 keys from HBM; rms error of a shape
+// 5 .. 10 %); the plan it picks is 1.6 % (fp32: 2.7) slower than the best measured one in the mean, 11 % (17) at most.  fp32 has tables of its
+// own: by bf16's it came out 3.4 % slower in the mean, 34 at most, as a tile takes it twice as long.  One wave is for few keys and many
+// rows: 4 sequences, 8 kv heads of 7, 160 rows, 32 keys take 8.7 us with one, 11.5 with four; 8 sequences, 28 / 4 heads, 256 rows, 128
+// keys 14.9 and 19.0.
 double q4_cost(const Q4Shape &sh, int64_t pairs, int64_t rows, int64_t tiles, int dh, int64_t splits)
 {
     const int64_t groups = (rows + 16 * sh.rt - 1) / (16 * sh.rt), per = (tiles + splits - 1) / splits;
@@ -487,8 +497,10 @@ FcQ4Plan plan(const FcQ4Geom &G, int A, int kv_len, size_t cap)
         return best;
     }
     double least = 1e30;
-    for (const Q4Shape &sh : G.Dh == 128 ? Q4_128 : Q4_64) {
-        if (sh.rt == 2 && G.dtype == FC_F32) continue;
+    const bool f32 = G.dtype == FC_F32;
+    const Q4Shape *const shapes = f32 ? (G.Dh == 128 ? Q4_F32_128 : Q4_F32_64) : G.Dh == 128 ? Q4_128 : Q4_64;
+    for (int i = 0; i < (f32 ? 4 : 6); ++i) {
+        const Q4Shape &sh = shapes[i];
         const int64_t groups = (rows + 16 * sh.rt - 1) / (16 * sh.rt);
         for (const int splits : SPLITS) {
             const FcQ4Plan pl{sh.rt, sh.waves, splits};
