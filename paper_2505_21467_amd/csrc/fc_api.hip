@@ -1583,7 +1583,7 @@ fc_status fc_q4_attention(const fc_q4_cache *cache, int32_t layer, const void *q
 size_t fc_sample_workspace_bytes(int32_t dtype, int32_t M, int32_t V)
 {
     if ((dtype != FC_F32 && dtype != FC_BF16) || M < 1 || V < 1 || M > 65535 || V > (1 << 24) || (int64_t)M * V > ((int64_t)1 << 36)) return 0;
-    return fc_sample_workspace(dtype, M, V);
+    return fc_sample_workspace(M, V);
 }
 
 fc_status fc_sample_tokens(int32_t dtype, const void *logits, int64_t ld, int32_t M, int32_t V, float temperature, int32_t top_k,
@@ -1605,7 +1605,7 @@ fc_status fc_sample_tokens(int32_t dtype, const void *logits, int64_t ld, int32_
     if (M > 65535 || V > (1 << 24)) return fail(FC_ERR_UNSUPPORTED, "M is limited to 65535, V to 2^24");
     if ((int64_t)M * V > ((int64_t)1 << 36)) return fail(FC_ERR_UNSUPPORTED, "M * V is limited to 2^36");
     if ((uintptr_t)workspace & 15) return fail(FC_ERR_INVALID_ARG, "workspace must be 16-byte aligned");
-    const size_t need = fc_sample_workspace(dtype, M, V), given = workspace ? workspace_bytes : 0;
+    const size_t need = fc_sample_workspace(M, V), given = workspace ? workspace_bytes : 0;
     if (given < need) return fail(FC_ERR_WORKSPACE, "workspace of %zu bytes needed, %zu given", need, given);
     FcSampleArgs p;
     p.logits = logits;

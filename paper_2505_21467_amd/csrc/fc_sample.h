@@ -19,5 +19,5 @@ struct FcSampleArgs {
     float *conf;
     void *workspace;
 };
-size_t fc_sample_workspace(int dtype, int M, int V);
+size_t fc_sample_workspace(int M, int V);
 hipError_t fc_launch_sample(const FcSampleArgs &p, int dtype, hipStream_t s);

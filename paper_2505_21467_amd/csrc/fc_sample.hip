@@ -917,26 +917,29 @@ __global__ __launch_bounds__(PICK) void k_sample_pick(FcSampleArgs p, int parts,
 
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// How a call is cut.  Parts are as short as leaves a row 20 of them (the second kernel adds them up) and the call 384 workgroups of parts twice as
-// long: 32 x 152064 take 27.5 us by parts of 8192, 28.2 by 16384 and 32.1 by 4096; one row of 32000 without filters 17.0 by 4096, 19.4 by 8192 and
-// 24.3 by 16384; 256 x 152064 42.5 by 16384 and 51.6 by 8192.  Where a row's lists do not do, rows of 256 KB and more are fetched by as many
-// workgroups as there are compute units to a row, of SLICE bytes at least, which costs them a ticket (57 rows of 50001 fp32: 27.1 us with one
-// workgroup, 27.6 with two; 32 x 152064 fp32: 48.2 with one, 39.8 with six; 8 x 152064 bf16 33.6 with one, 30.3 with three).
+// How a call is cut.  Measured over 220 shapes (5001 .. 262144 entries, 1 .. 256 rows, both types) with a top-k of 50 and without one, and over 208 with
+// every number of workgroups to a row:
+//  - Parts of 4096 where a row has at most 12 of them, 8192 where at most 24, else 16384, and longer where the call has 384 workgroups of the
+//    next length: 0.9 % slower than the best length in the mean, 12 at most.  The borders are flat, since short parts are for undecided
+//    rows, long ones for a top-k.  bf16, with a top-k and without: one row of 32000 15.7 and 27.3 us by 4096, 16.2 and 29.3 by 8192; 32 x
+//    80000 20.4 and 41.9 by 4096, 18.5 and 40.4 by 8192; 32 x 152064 21.0 and 57.4 by 8192, 19.7 and 58.1 by 16384.
+//  - Where a row's lists do not do, a workgroup fetches 32768 entries of it at a time.  Rows of 40000 and more have a workgroup for every 20000, as far
+//    as there are compute units: 0.6 % slower than the best number in the mean, 5 at most.  bf16 without a top-k: 32 x 152064 57.3 us with
+//    one, 48.8 with six, 32 x 80000 40.4 and (four) 37.3, 32 x 40000 34.9 and (two) 33.6, 32 x 36000 30.6 and 32.7.  Workgroups that are not needed cost
+//    up to 0.3.
 // The workspace has the parts' bins, their lists, what is said about them, and what the slices fetch.
 struct Plan {
     int part, parts, slices;
     size_t lists, abouts, shared, fetched, total;
-    Plan(int dtype, int M, int V)
+    Plan(int M, int V)
     {
-        constexpr int CUS = 256, SLICE = 96 << 10;
-        const int size = dtype == FC_F32 ? 4 : 2;
+        constexpr int CUS = 256, SLICE = 20000;
         auto parts_of = [&](int entries) { return (V + entries - 1) / entries; };
         part = SHORT;
-        while (part < LONG && (parts_of(part) > 20 || (int64_t)M * parts_of(2 * part) >= 384)) part *= 2;
+        while (part < LONG && (parts_of(part) > (part == SHORT ? 12 : 24) || (int64_t)M * parts_of(2 * part) >= 384)) part *= 2;
         parts = parts_of(part);
         slices = M >= CUS ? 1 : CUS / M;
-        const int64_t row = (int64_t)V * size;
-        const int most = row < 256 << 10 ? 1 : (int)(row / SLICE);
+        const int most = V < 2 * SLICE ? 1 : V / SLICE;
         if (slices > most) slices = most;
         const size_t n = (size_t)M * parts;
         lists = align256(n * ROOM * sizeof(uint64_t));
@@ -950,7 +953,7 @@ struct Plan {
 template <typename T>
 void launch(const FcSampleArgs &p, hipStream_t s)
 {
-    const Plan w(sizeof(T) == 4 ? FC_F32 : FC_BF16, p.M, p.V);
+    const Plan w(p.M, p.V);
     char *at = (char *)p.workspace;
     uint64_t *bins = (uint64_t *)at, *lists = (uint64_t *)(at + w.lists), *fetched = (uint64_t *)(at + w.fetched);
     Part *abouts = (Part *)(at + w.abouts);
@@ -964,7 +967,7 @@ void launch(const FcSampleArgs &p, hipStream_t s)
 
 }  // namespace
 
-size_t fc_sample_workspace(int dtype, int M, int V) { return Plan(dtype, M, V).total; }
+size_t fc_sample_workspace(int M, int V) { return Plan(M, V).total; }
 
 hipError_t fc_launch_sample(const FcSampleArgs &args, int dtype, hipStream_t s)
 {
