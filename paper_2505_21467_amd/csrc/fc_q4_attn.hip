@@ -11,7 +11,7 @@
 //    the result, and four take as long as the conversions.  As two 8-bit numbers its products would be cut off at 2^-14 of their sum.)
 //  - Weights.  Value row t is codes times 2^e_t.  The power goes into the exponent of the row's weight, w_t = 2^(s_t + e_t - r), so the codes
 //    are multiplied as they are, and the sum that divides adds w_t 2^-e_t.  The key multiply starts from e_t over the softmax scale, so this
-//    costs nothing.  The reference r only has to keep w_t in range: it is set 2^7 below the largest and moves when a score passes it by 2^15, which after
+//    costs nothing.  The reference r only has to keep w_t in range: it is set 2^7 below the largest and moves when a score passes it by 2^14, which after
 //    the first tiles is rare.  Weights are rounded to fp16: 11 bits down to 2^-21 of the largest, none below 2^-32 (half a step of the least
 //    number; the sum that divides has them all, in fp32).  bfloat16 would add as much error as rounding the output does, two E2M3 parts
 //    more, 2.8e-3 for 1.7e-3 relative in all.  Sums are fp32.
@@ -41,7 +41,8 @@ typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 
 constexpr float LIFT = 7.f;   // a row's largest weight so far is 2^LIFT when its reference is set
-constexpr float MOVE = 15.f;  // and none may pass 2^MOVE: fp16 ends at 65504
+constexpr float MOVE = 14.f;  // and none may pass 2^MOVE but for roundings: fp16 ends at 65504 (fp32: half its step there, 8, times FINE does too)
+constexpr float HUGE_REF = 0x1p20f;  // from here on the roundings of a score decide weights
 constexpr float FINE = 4096.f;  // fp32: what a weight's fp16 lacks is multiplied in units of 1 / FINE
 template <typename T> constexpr int MOST_RT = sizeof(T) == 4 ? 1 : 2;  // row tiles of a workgroup
 
@@ -177,6 +178,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
 
     f4 o[DT][RT], fine[FULL ? DT : 1][RT];
     float ref[RT], sum[RT];
+    bool huge = false;  // a reference whose roundings count
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         ref[rt] = -__builtin_inff();
@@ -252,7 +254,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
             } else {
                 top[rt] = max16(s[rt]) * p.c;
             }
-            move |= top[rt] > ref[rt] + MOVE;
+            move |= top[rt] - ref[rt] > MOVE;
         }
         if (__any(move)) {
 #pragma unroll
@@ -268,7 +270,25 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
                     o[dt][rt] *= a;
                     if constexpr (FULL) fine[dt][rt] *= a;
                 }
+                huge |= __any(fabsf(r) > HUGE_REF);
             }
+        }
+        // A weight's exponent.  Where the scores are so large that the product with the scale is off by what decides a weight, it is rounded as the
+        // largest's was, which the reference comes from: none then passes that one, and the largest is not lost.
+        if (__builtin_expect(!huge, 1)) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[rt][i / 4][i % 4] = fmaf(s[rt][i / 4][i % 4], p.c, FULL ? start[i / 4][i % 4] - ref[rt] : -ref[rt]);
+        } else {
+#pragma clang fp contract(off)
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float x = FULL ? fmaf(s[rt][i / 4][i % 4], p.c, start[i / 4][i % 4]) : s[rt][i / 4][i % 4] * p.c;
+                    s[rt][i / 4][i % 4] = x - ref[rt];
+                }
         }
         h8 w[RT][2], rest[RT][2];
 #pragma unroll
@@ -278,7 +298,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
             for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) {
-                    const float x = __builtin_amdgcn_exp2f(fmaf(s[rt][i][k], p.c, FULL ? start[i][k] - ref[rt] : -ref[rt]));
+                    const float x = __builtin_amdgcn_exp2f(s[rt][i][k]);
                     sum[rt] = fmaf(x, f[k], sum[rt]);
                     w[rt][i / 2][i % 2 * 4 + k] = (_Float16)x;
                     if constexpr (FULL) rest[rt][i / 2][i % 2 * 4 + k] = (_Float16)((x - (float)(_Float16)x) * FINE);
