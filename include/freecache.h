@@ -220,8 +220,8 @@ fc_status fc_refresh(fc_cache *cache, int32_t layer, const void *x, const void *
 /* ---------------------------------------------------------------------------------------------
  * A cache held in 4 bits, and the attention that reads it.  The rows of the prompt and of finished blocks are written once and
  * read by every later step; at 4 bits per value a step reads 133 bytes per row, kv head and K/V pair of head_dim 128 in place of
- * 512.  A step over it projects into a full-precision fc_cache of ONE layer that all layers share, moves the fresh rows over and
- * attends here:
+ * 512.  A step over it projects into a full-precision fc_cache of ONE layer that all layers share, moves the fresh rows over,
+ * which rounds them to 4 bits as well, and attends here:
  *   fc_qkv_project_scatter(one, 0, ...);  fc_q4_store_from(q4, layer, one, 0, ...);  fc_q4_attention(q4, layer, ...)
  *
  * Format.  A value is an E2M1 number (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) times a power of two 2^e.  Keys: one e per
@@ -252,18 +252,18 @@ fc_status fc_q4_free(fc_q4_cache *cache);
  *   k_rows, v_rows  device [B][Hkv][rows][Dh]
  *   pos  device int32 [B][rows] or NULL.  A negative entry, or one >= max_seq, marks a padded row: it is not stored.  Where a sequence
  *        lists a place twice the later row is stored.
- * Errors: INVALID_ARG, BOUNDS (layer; with pos == NULL: start < 0 or start + rows > max_seq), HIP. */
+ * Errors: INVALID_ARG, BOUNDS (layer; with pos == NULL: start < 0 or start + rows > max_seq), UNSUPPORTED (rows beyond 2^24), HIP. */
 fc_status fc_q4_store_rows(fc_q4_cache *cache, int32_t layer, const void *k_rows, const void *v_rows, const int32_t *pos,
                            int32_t start, int32_t rows, void *stream);
 
 /* Store rows out of a layer of a full-precision cache, each to its own place: the rows pos[b][r], or start + r when pos is NULL.
  * src has the same batch, n_kv_heads, head_dim, max_seq and dtype.
- * Errors: INVALID_ARG (also: another geometry), BOUNDS, HIP. */
+ * Errors: INVALID_ARG (also: another geometry), BOUNDS, UNSUPPORTED, HIP. */
 fc_status fc_q4_store_from(fc_q4_cache *cache, int32_t layer, const fc_cache *src, int32_t src_layer, const int32_t *pos,
                            int32_t start, int32_t rows, void *stream);
 
 /* Rows [start, start+rows) as the values they stand for (exact in either dtype), k_rows, v_rows device [B][Hkv][rows][Dh].
- * Errors: INVALID_ARG, BOUNDS, HIP. */
+ * Errors: INVALID_ARG, BOUNDS, UNSUPPORTED, HIP. */
 fc_status fc_q4_read_rows(const fc_q4_cache *cache, int32_t layer, void *k_rows, void *v_rows, int32_t start, int32_t rows,
                           void *stream);
 
