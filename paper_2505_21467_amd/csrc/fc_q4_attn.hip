@@ -270,7 +270,7 @@ __global__ __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(2))) voi
                     o[dt][rt] *= a;
                     if constexpr (FULL) fine[dt][rt] *= a;
                 }
-                huge |= __any(fabsf(r) > HUGE_REF);
+                huge |= __any(fabsf(r) > HUGE_REF && fabsf(r) < __builtin_inff());  // (rows that are not numbers change no other's bits)
             }
         }
         // A weight's exponent.  Where the scores are so large that the product with the scale is off by what decides a weight, it is rounded as the

@@ -43,3 +43,17 @@ def test_one_key_takes_everything(dtype, Dh, e, n):
             compared += 1
             assert (got[0, a, h] >= lo - off).all() and (got[0, a, h] <= hi + off).all(), (h, a, got[0, a, h][:4], lo[:4], hi[:4])
     assert compared >= 20 or e < 24
+
+
+@pytest.mark.parametrize("dtype,Dh", [("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), -float("inf")])
+def test_rows_that_are_not_numbers_change_no_others_bits(dtype, Dh, what):
+    c = Cache(dtype, 1, 2, 1, Dh, 400)
+    c.store(*c.rows(92, 400))
+    q = inputs.normal(93, "q", (1, 2, 12, Dh), 1.5, dtype).clone()
+    want = c.attend(q, 400)
+    q[0, 1, 4, 9] = what
+    got = c.attend(q, 400)
+    other = np.ones((12, 2), bool)
+    other[4, 1] = False
+    assert np.array_equal(got[0][other], want[0][other]) and np.isnan(got[0, 4, 1]).all()
